@@ -10,7 +10,8 @@
  *     sushi_set_subgraph_cache   every Q   make a SubGraph's weights resident
  *     sushi_infer                per query run one SubNet, logits out
  *
- * plus the host-side scheduler of Algorithm 1 (sushi_sched_*) and counters (sushi_get_stats).
+ * plus the host-side scheduler of Algorithm 1 (sushi_sched_*), counters (sushi_get_stats) and operators on the logits that
+ * queries leave on the device (sushi_sample, sushi_top_logits, sushi_distill).
  *
  * Conventions
  *   - Plain C types only.  Every pointer is marked HOST or DEVICE below.
@@ -322,6 +323,91 @@ int sushi_infer(sushi_ctx *ctx, const sushi_subnet_cfg *cfg, const void *input_d
  *   - The SubGraph cache has no effect on this path (as in exec mode 0); the counters are kept. */
 #define SUSHI_STATIC_SCRATCH_BYTES (16u << 20)
 int sushi_infer_static(sushi_ctx *ctx, const sushi_subnet_cfg *cfg, const void *input_dev, int batch, void *logits_dev);
+
+/* ---------------------------------------------------------------- operators on logits
+ *
+ * What follows a query: an answer drawn from its logits, its leading classes, the distance of a SubNet's answers from the
+ * largest SubNet's and that distance's gradient.  They need a context with a device but no SuperNet, take any rows of logits
+ * (sushi_infer's are float32 with row_stride = n_classes), enqueue on the context's stream, allocate nothing and may be
+ * captured into a HIP graph (not with SUSHI_OPT_KERNEL_TIMING on).  In exec mode 3 call sushi_synchronize between a query and
+ * the operator that reads its logits; as every other kernel, the operator's wait while the team kernel fills the GPU.
+ *
+ * The order of a row: value descending, then class index ascending.  -inf marks a class that is not there (masked, padding): it
+ * is in no order and has no probability.  sushi_sample and sushi_top_logits read NaN as -inf; sushi_distill passes it on.
+ * Where a row holds +inf, its infinite logits share the row's probability.  rows = 0 is allowed and does nothing.
+ *
+ * workspace: DEVICE, 16-byte aligned, at least sushi_logits_workspace() bytes for the same rows and classes.  Its contents mean
+ * nothing before and after a call.  Calls whose work may overlap in time (other streams, graphs replayed side by side) need
+ * one each.  Outputs must not overlap inputs, except where it is said; strides and everything but workspace sizes are in
+ * elements.  DEVICE pointers must be aligned to their element. */
+#define SUSHI_MAX_CLASSES (1 << 20) /* classes of a row, here */
+#define SUSHI_MAX_TOP 1024          /* entries of a list of leading classes */
+
+typedef struct sushi_logits {
+    const void *data;   /* DEVICE, [rows][classes] */
+    int32_t dtype;      /* sushi_dtype: SUSHI_FP32 or SUSHI_BF16 */
+    int32_t rows;
+    int32_t classes;    /* 1 .. SUSHI_MAX_CLASSES */
+    int64_t row_stride; /* elements from row to row, at least classes */
+} sushi_logits;
+
+/* Host only.  SUSHI_EINVAL for rows < 0 or classes outside 1 .. SUSHI_MAX_CLASSES. */
+int sushi_logits_workspace(int32_t rows, int32_t classes, size_t *n_bytes);
+
+/* How sushi_sample draws.  Every array DEVICE, one entry per row, or NULL. */
+typedef struct sushi_sampling {
+    const float *temperature; /* T: the probabilities are softmax(logits / T).  <= 0 or NaN: the row's answer is the first of its
+                                 order, whatever else is set.  NULL: 1 */
+    const int32_t *top_k;     /* keep the first top_k classes of the order.  <= 0, NULL: all */
+    const float *top_p;       /* keep a class if the classes before it in the order have less than top_p of the probability (the
+                                 first is always kept).  >= 1, NaN, NULL: all */
+    const float *min_p;       /* keep a class if its probability is at least min_p (at most 1 is used) times the largest.  <= 0,
+                                 NaN, NULL: all */
+} sushi_sampling;
+
+/* Draws one class per row from given random numbers.  A class is a candidate if every filter keeps it; all three look at the
+ * probabilities of the whole row.  The answer is the lowest class index at which the candidates' probability, summed in the
+ * order of the class indexes, exceeds u times that of all candidates.  Weights and sums have 64 bits.
+ *   uniform   DEVICE [rows], u in [0, 1) (what lies outside is taken as the nearest float32 in it; NaN: 0)
+ *   sampling  may be NULL (a plain draw)
+ *   classes   DEVICE int32 [rows]; -1 for a row without a logit above -inf
+ *   log_prob  DEVICE float32 [rows] or NULL: ln of the answer's probability among the candidates; 0 where T chose the first,
+ *             -inf with class -1 */
+int sushi_sample(sushi_ctx *ctx, const sushi_logits *logits, const sushi_sampling *sampling, const float *uniform,
+                 int32_t *classes, float *log_prob, void *workspace, size_t workspace_bytes);
+
+/* The first k classes of each row's order, 1 <= k <= min(classes, SUSHI_MAX_TOP): what a teacher leaves for sushi_distill.
+ *   values   DEVICE float32 [rows][k], descending; -inf where the row has fewer logits above -inf
+ *   classes  DEVICE int32 [rows][k]; -1 there
+ *   rest     DEVICE float32 [rows] or NULL: the probability, softmax(logits / temperature), of the classes not listed (summed by
+ *            itself: exact where it is small; 0 for a row without a logit above -inf)
+ * temperature: positive and finite. */
+int sushi_top_logits(sushi_ctx *ctx, const sushi_logits *logits, int k, float temperature, float *values, int32_t *classes,
+                     float *rest, void *workspace, size_t workspace_bytes);
+
+/* A teacher's leading logits for the rows of a student. */
+typedef struct sushi_teacher {
+    const float *values;    /* DEVICE [rows][k] logits, in any order */
+    const int32_t *classes; /* DEVICE [rows][k]; an entry whose class is outside [0, classes) or stands in an earlier entry of the row is
+                               skipped */
+    const float *rest;      /* DEVICE [rows]: the teacher's probability outside the list (moved into [0, 1]), or NULL: 0 */
+    int32_t k;              /* 1 .. SUSHI_MAX_TOP */
+} sushi_teacher;
+
+/* Distillation: with q = softmax(logits / T) of the student, p = (1 - rest) * softmax(values / T) over the row's entries and the
+ * classes that are not listed taken as one class of probability `rest` and q_rest,
+ *     loss = sum_i p_i (ln p_i - ln q_i) + rest (ln rest - ln q_rest)                      (0 ln 0 = 0)
+ *     d loss / d logit_j = (q_j - p_j) / T for a listed class, q_j (1 - rest / q_rest) / T for another.
+ *   loss         DEVICE float32 [rows] or NULL
+ *   grad         DEVICE, type of the logits, [rows][grad_stride], or NULL (forward only): weight[row] times the gradient of the
+ *                row's loss.  May be the student's own memory (same address, same stride); other overlaps are refused.  What lies
+ *                between classes and grad_stride is not written
+ *   weight       DEVICE float32 [rows] (the gradient of the whole by the row's loss) or NULL: 1; 0 makes the row's gradient zero
+ *                whatever the row holds
+ * A row without an entry whose value is above -inf, or without a logit above -inf, has loss 0 and gradient 0.  A listed class that the
+ * student gives -inf makes the loss +inf (if its p is not 0).  temperature: positive and finite. */
+int sushi_distill(sushi_ctx *ctx, const sushi_logits *student, const sushi_teacher *teacher, float temperature,
+                  const float *weight, float *loss, void *grad, int64_t grad_stride, void *workspace, size_t workspace_bytes);
 
 /* Waits until every query enqueued or posted through ctx has finished and its logits are visible
  * to the host and to later work on any stream. */

@@ -97,6 +97,19 @@ class CLaunchRecord(C.Structure):
                 ("bytes", C.c_double), ("flops", C.c_double)]
 
 
+class CLogits(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("classes", C.c_int32),
+                ("row_stride", C.c_int64)]
+
+
+class CSampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class CTeacher(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("classes", C.c_void_p), ("rest", C.c_void_p), ("k", C.c_int32)]
+
+
 _lib = None
 
 
@@ -137,6 +150,10 @@ def lib():
     L.sushi_set_option.argtypes = [vp, C.c_int, C.c_int64]
     L.sushi_get_kernel_stats.argtypes = [vp, C.POINTER(CKernelStats), C.c_int, ip]
     L.sushi_get_launch_records.argtypes = [vp, C.POINTER(CLaunchRecord), C.c_int, ip]
+    L.sushi_logits_workspace.argtypes = [C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+    L.sushi_sample.argtypes = [vp, C.POINTER(CLogits), C.POINTER(CSampling), vp, vp, vp, vp, C.c_size_t]
+    L.sushi_top_logits.argtypes = [vp, C.POINTER(CLogits), C.c_int, C.c_float, vp, vp, vp, vp, C.c_size_t]
+    L.sushi_distill.argtypes = [vp, C.POINTER(CLogits), C.POINTER(CTeacher), C.c_float, vp, vp, vp, C.c_int64, vp, C.c_size_t]
     _lib = L
     return L
 
@@ -225,6 +242,15 @@ def sushi_team_plan(arch, cfg, batch, team_wgs):
     return [{f: getattr(buf[i], f) for f, _ in CTeamOp._fields_} for i in range(n.value)]
 
 
+def sushi_logits_workspace(rows, classes):
+    """Bytes of workspace that the operators on logits need for rows of so many classes (host only)."""
+    n = C.c_size_t(0)
+    rc = lib().sushi_logits_workspace(int(rows), int(classes), C.byref(n))
+    if rc != 0:
+        raise SushiError(rc, "logits_workspace: bad shape")
+    return n.value
+
+
 def marshal_box(box):
     """(K, C, r) triples -> sushi_layer_dims array."""
     return (CLayerDims * len(box))(*[CLayerDims(k, c, r) for (k, c, r) in box])
@@ -240,6 +266,13 @@ def sushi_subgraph_overlap(subnet_box, subgraph_box, bytes_per_weight=2):
     return total.value, common.value, hit.value
 
 
+EINVAL = -1
+
+
+def _refuse(what):
+    raise SushiError(EINVAL, what)
+
+
 class Sushi:
     """One context (device + stream)."""
 
@@ -253,6 +286,7 @@ class Sushi:
         rc = lib().sushi_create(C.byref(self._h), device, C.c_void_p(stream))
         if rc != 0:
             raise SushiError(rc, (lib().sushi_last_error(None) or b"").decode())
+        self.device = device
         self.arch = None
         self.dtype = None
         self._cfg_cache = {}
@@ -359,6 +393,78 @@ class Sushi:
         if rc != 0:
             _check(rc, self._h)
         return self._j.value
+
+    # Operators on logits.  Device tensors in and out, as in sushi_infer: nothing is allocated, copied or converted here.
+    # What the C call cannot see of a tensor (its device, its type, its strides) is checked first.
+    def _operand(self, t, what, dtype, shape):
+        """Address of a contiguous tensor of that type (a name) and shape; None: NULL."""
+        if t is None:
+            return None
+        if str(t.dtype) != "torch." + dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            _refuse("%s: a contiguous %s tensor of shape %s is needed" % (what, dtype, list(shape)))
+        if not t.is_cuda or t.device.index != self.device:
+            _refuse("%s: not on the context's device" % what)
+        return t.data_ptr()
+
+    def _rows(self, t, what):
+        """(sushi_logits, type's name) of a tensor [rows, classes] whose rows are contiguous."""
+        name = str(t.dtype)[len("torch."):]
+        if name not in ("float32", "bfloat16") or t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+            _refuse("%s: a float32 or bfloat16 tensor [rows, classes] with contiguous rows is needed" % what)
+        if not t.is_cuda or t.device.index != self.device:
+            _refuse("%s: not on the context's device" % what)
+        rows, classes = t.shape
+        stride = t.stride(0) if rows > 1 else max(t.stride(0), classes)
+        return CLogits(t.data_ptr(), BF16 if name == "bfloat16" else FP32, rows, classes, stride), name
+
+    def _workspace(self, t):
+        if t is None:
+            return None, 0
+        if not t.is_cuda or t.device.index != self.device or not t.is_contiguous():
+            _refuse("workspace: a contiguous tensor on the context's device is needed")
+        return t.data_ptr(), t.numel() * t.element_size()
+
+    def sushi_sample(self, logits, uniform, classes, log_prob=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                     workspace=None):
+        """One class per row of logits [rows, classes], drawn with the random numbers uniform [rows] (float32).  classes: int32
+        [rows] out; log_prob: float32 [rows] out or None; temperature, top_p, min_p (float32), top_k (int32): [rows] or None."""
+        z, _ = self._rows(logits, "logits")
+        n = (z.rows,)
+        s = CSampling(self._operand(temperature, "temperature", "float32", n), self._operand(top_k, "top_k", "int32", n),
+                      self._operand(top_p, "top_p", "float32", n), self._operand(min_p, "min_p", "float32", n))
+        _check(lib().sushi_sample(self._h, C.byref(z), C.byref(s), self._operand(uniform, "uniform", "float32", n),
+                                  self._operand(classes, "classes", "int32", n), self._operand(log_prob, "log_prob", "float32", n),
+                                  *self._workspace(workspace)), self._h)
+
+    def sushi_top_logits(self, logits, values, classes, rest=None, temperature=1.0, workspace=None):
+        """The k leading logits of every row: values (float32) and classes (int32) [rows, k] out, rest (float32 [rows]) out or
+        None: the probability outside them at the temperature."""
+        z, _ = self._rows(logits, "logits")
+        if values is None or values.dim() != 2:
+            _refuse("values: a float32 tensor [rows, k] is needed")
+        shape = (z.rows, values.shape[1])
+        _check(lib().sushi_top_logits(self._h, C.byref(z), shape[1], temperature, self._operand(values, "values", "float32", shape),
+                                      self._operand(classes, "classes", "int32", shape),
+                                      self._operand(rest, "rest", "float32", (z.rows,)), *self._workspace(workspace)), self._h)
+
+    def sushi_distill(self, student, values, classes, loss, rest=None, temperature=1.0, weight=None, grad=None, workspace=None):
+        """Loss of every row of student [rows, classes] against a teacher's list values (float32), classes (int32) [rows, k] with
+        probability rest [rows] (None: 0) outside it: loss float32 [rows] out or None; grad (type and shape of student, rows
+        contiguous; student itself is allowed) out or None: weight [rows] (None: 1) times the gradient."""
+        z, name = self._rows(student, "student")
+        if values is None or values.dim() != 2:
+            _refuse("values: a float32 tensor [rows, k] is needed")
+        shape, n = (z.rows, values.shape[1]), (z.rows,)
+        t = CTeacher(self._operand(values, "values", "float32", shape), self._operand(classes, "classes", "int32", shape),
+                     self._operand(rest, "rest", "float32", n), shape[1])
+        g = CLogits()
+        if grad is not None:
+            g, grad_name = self._rows(grad, "grad")
+            if grad_name != name or tuple(grad.shape) != tuple(student.shape):
+                _refuse("grad: the type and shape of student are needed")
+        _check(lib().sushi_distill(self._h, C.byref(z), C.byref(t), temperature, self._operand(weight, "weight", "float32", n),
+                                   self._operand(loss, "loss", "float32", n), g.data, g.row_stride, *self._workspace(workspace)),
+               self._h)
 
     def sushi_synchronize(self):
         _check(lib().sushi_synchronize(self._h), self._h)

@@ -170,7 +170,10 @@ enum KernelClass {
     KC_SE_GATE = 16,    // se_gate_kernel (both fully connected layers of a squeeze-excite block)
     KC_EXPAND_DW = 17,  // expand_dw_kernel (1x1 expansion and depthwise layer)
     KC_CONV_KSPLIT = 18,  // conv_ksplit_kernel (3x3, the reduction split over the waves of a workgroup)
-    KC_COUNT = 19
+    KC_SAMPLE = 19,     // sushi_sample, sushi_top_logits, sushi_distill (one entry per call)
+    KC_TOP_LOGITS = 20,
+    KC_DISTILL = 21,
+    KC_COUNT = 22
 };
 const char *kernel_class_name(int kc);
 

@@ -492,7 +492,8 @@ const char *kernel_class_name(int kc) {
                                           "conv_patch_kernel",  "conv_i8_direct_kernel", "int8_pool_fc_kernels",
                                           "stem_mfma_kernel",   "conv_tile_kernel",    "dw_mfma_kernel",
                                           "dwconv_kernel",      "se_gate_kernel",     "expand_dw_kernel",
-                                          "conv_ksplit_kernel"};
+                                          "conv_ksplit_kernel", "sample_kernels",     "top_logits_kernels",
+                                          "distill_kernels"};
     return kc >= 0 && kc < KC_COUNT ? names[kc] : "?";
 }
 

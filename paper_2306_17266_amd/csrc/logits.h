@@ -1,0 +1,74 @@
+// Operators on rows of logits (row_order.hip, distill.hip): what their launchers take.
+//
+// The order of a row: value descending, index ascending; a NaN counts as -inf, and what is -inf belongs to no order.
+// The weight of a logit: exp((z - max z) / T).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace sushi {
+
+constexpr int LOGITS_MAX_CLASSES = 1 << 20;  // (so that sums of weights fit 64-bit fixed point, and indexes of 16-byte pieces an int)
+constexpr int LOGITS_MAX_TOP = 1024;
+
+struct LogitRows {
+    const void *x;  // float32 or bf16
+    long stride;    // elements from row to row
+    int rows, n;    // n logits in a row
+    bool bf16;
+};
+
+struct SampleArgs {
+    LogitRows in;
+    const float *uniform;      // [rows]
+    const float *temperature;  // [rows] or null (1); this and the next three
+    const int32_t *top_k;      // (null, <= 0: all)
+    const float *top_p;        // (null, >= 1, NaN: all)
+    const float *min_p;        // (null, <= 0, NaN: all)
+    int32_t *classes;          // [rows]
+    float *log_prob;           // [rows] or null
+};
+
+struct TopArgs {
+    LogitRows in;
+    int k;
+    float temperature;  // of `rest`
+    float *values;      // [rows][k]
+    int32_t *classes;   // [rows][k]
+    float *rest;        // [rows] or null
+};
+
+struct DistillArgs {
+    LogitRows in;
+    const float *values;     // [rows][k]
+    const int32_t *classes;  // [rows][k]
+    const float *rest;       // [rows] or null (0)
+    const float *weight;     // [rows] or null (1)
+    int k;
+    float temperature;
+    float *loss;       // [rows] or null
+    void *grad;        // type of the logits, or null
+    long grad_stride;  // elements from row to row
+};
+
+// Pieces of 16 bytes that a workgroup of the kernels for parts of rows takes, and parts that go out in one launch (what a
+// call needs of the workspace stays bounded).
+constexpr int LOGITS_PART_PIECES = 2048;
+constexpr long LOGITS_SLICE = 1 << 20;
+inline int logits_parts(int n, bool bf16) {  // (a row may start inside its first piece)
+    const int per = bf16 ? 8 : 4;
+    return ((n + 2 * per - 2) / per + LOGITS_PART_PIECES - 1) / LOGITS_PART_PIECES;
+}
+
+// Bytes of scratch memory that every operator gets by with on rows of n logits.
+size_t logits_workspace_bytes(int rows, int n);
+
+// Return hipSuccess or the launch error.  ws: logits_workspace_bytes() bytes, 16-byte aligned.
+hipError_t launch_sample(const SampleArgs &a, void *ws, hipStream_t s);
+hipError_t launch_top_logits(const TopArgs &a, void *ws, hipStream_t s);
+hipError_t launch_distill(const DistillArgs &a, void *ws, hipStream_t s);
+
+}  // namespace sushi

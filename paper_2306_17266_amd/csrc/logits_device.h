@@ -1,0 +1,169 @@
+// Device-side helpers of the operators on logits: access to a row, order keys, weights, sums over waves and workgroups.
+#pragma once
+
+#include "device_common.h"
+#include "logits.h"
+
+namespace sushi {
+
+// ------------------------------------------------------------------ order and weight of a logit
+
+// Unsigned numbers in the order of the logits: larger = earlier.  NaN as -inf, -0 as 0.
+constexpr uint32_t KEY_NONE = 0x007FFFFFu;  // of -inf: in no order
+__device__ __forceinline__ uint32_t order_key(float z) {
+    z = z == z ? z + 0.0f : -INFINITY;
+    const uint32_t u = __float_as_uint(z);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+// 2^t for t <= 0 in 64 bits: t = i + f with |f| <= 1/2, the power series of 2^f up to f^DEGREE (what is left out: 2e-14 of the
+// value at most with degree 11, 5e-9 with 7), and i into the exponent.  Below 2^-1022, for -inf and for NaN: zero.
+template <int DEGREE>
+__device__ __forceinline__ double exp2_64(double t) {
+    t = fmax(t, -1100.0);
+    const double i = __builtin_rint(t), f = t - i;
+    // (ln 2)^n / n!
+    constexpr double c[12] = {1.0,
+                              6.931471805599453094e-01,
+                              2.402265069591007123e-01,
+                              5.550410866482157995e-02,
+                              9.618129107628477162e-03,
+                              1.333355814642844343e-03,
+                              1.540353039338160995e-04,
+                              1.525273380405984028e-05,
+                              1.321548679014430949e-06,
+                              1.017808600923969973e-07,
+                              7.054911620801123330e-09,
+                              4.445538271870811498e-10};
+    double p = c[DEGREE];
+#pragma unroll
+    for (int n = DEGREE - 1; n >= 0; --n) p = fma(p, f, c[n]);
+    return ldexp(p, (int)i);
+}
+
+// Weights of a row's logits at a temperature.  With an infinite maximum the limit: the infinite ones share the row.
+struct Weight {
+    double best, scale;  // maximum; log2(e) / T
+    bool infinite;
+    __device__ __forceinline__ Weight(float m, double inv_t) : best(m), scale(inv_t * 1.4426950408889634074), infinite(m == INFINITY) {}
+    __device__ __forceinline__ double log2_of(float z) const {  // <= 0, or NaN for what has no weight
+        if (infinite) return z == INFINITY ? 0.0 : -INFINITY;
+        return ((double)z - best) * scale;
+    }
+};
+
+// ------------------------------------------------------------------ a row
+
+template <typename T>
+__device__ __forceinline__ void unpack(uint4 r, float (&v)[16 / sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) {
+        v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y), v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
+    } else {
+        v[0] = bf2f(r.x & 0xFFFFu), v[1] = __uint_as_float(r.x & 0xFFFF0000u), v[2] = bf2f(r.y & 0xFFFFu), v[3] = __uint_as_float(r.y & 0xFFFF0000u);
+        v[4] = bf2f(r.z & 0xFFFFu), v[5] = __uint_as_float(r.z & 0xFFFF0000u), v[6] = bf2f(r.w & 0xFFFFu), v[7] = __uint_as_float(r.w & 0xFFFF0000u);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(T)]) {
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else
+        return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+
+// One row, or a part of it, as a workgroup reads it: in pieces of 16 bytes at 16-byte addresses (the first and the last may be partly outside the
+// row, whose start need not be aligned: what is outside is not loaded and reads as -inf).  Every wave has a run of pieces of
+// its own, so that the order of (wave, round, lane, element) is the order of the indexes; neighbouring lanes have
+// neighbouring pieces.
+template <typename T>
+struct Row {
+    static constexpr int PER = 16 / sizeof(T);  // logits of a piece
+    const T *x;
+    int n, lead;        // logits; elements of the first piece before the row
+    int first, rounds;  // this lane's first piece, and how many it has (64 apart)
+
+    // A part: `most` pieces, a multiple of 64 * waves, from piece `from` on.
+    __device__ __forceinline__ Row(const LogitRows &in, long row, int wave, int waves, int lane, int from = 0, int most = 0x7FFFFFFF) {
+        x = static_cast<const T *>(in.x) + row * in.stride;
+        n = in.n;
+        lead = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+        const int pieces = min((n + lead + PER - 1) / PER - from, most);
+        rounds = pieces > 0 ? (pieces + 64 * waves - 1) / (64 * waves) : 0;
+        first = from + wave * rounds * 64 + lane;
+    }
+    __device__ __forceinline__ int index(int i) const { return (first + i * 64) * PER - lead; }  // of the piece's first element
+    __device__ __forceinline__ uint4 load(int i) const {
+        const int j = index(i);
+        if (j >= 0 && j + PER <= n) return *reinterpret_cast<const uint4 *>(x + j);
+        constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+        uint32_t w[4] = {none, none, none, none};
+        if (j + PER > 0 && j < n) {
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (j + e >= 0 && j + e < n) {
+                    if constexpr (sizeof(T) == 4)
+                        w[e] = __float_as_uint(x[j + e]);
+                    else
+                        w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | (uint32_t)x[j + e] << 16 : (w[e / 2] & 0xFFFF0000u) | x[j + e];
+                }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // f(logit, index) for every element of this lane's i-th piece, of all its pieces
+    template <typename F>
+    __device__ __forceinline__ void piece(int i, F f) const {
+        float v[PER];
+        unpack<T>(load(i), v);
+        const int j = index(i);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) f(v[e], j + e);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        for (int i = 0; i < rounds; ++i) piece(i, f);
+    }
+};
+
+// ------------------------------------------------------------------ sums over a wave and a workgroup (the same in every run)
+
+template <typename V, typename F>
+__device__ __forceinline__ V wave_all(V v, F f) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ V wave_sum(V v) {
+    return wave_all(v, [](V a, V b) { return a + b; });
+}
+// Sum over this lane and those before it.
+template <typename V>
+__device__ __forceinline__ V wave_scan(V v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const V u = __shfl_up(v, d);
+        v += lane >= d ? u : V(0);
+    }
+    return v;
+}
+
+// f over all threads of the workgroup.  part: LDS, one entry per wave; free again after the next barrier.
+template <int THREADS, typename V, typename F>
+__device__ __forceinline__ V block_all(V v, V *part, F f) {
+    v = wave_all(v, f);
+    if (THREADS == 64) return v;
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    V r = part[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) r = f(r, part[w]);
+    return r;
+}
+template <int THREADS, typename V>
+__device__ __forceinline__ V block_sum(V v, V *part) {
+    return block_all<THREADS>(v, part, [](V a, V b) { return a + b; });
+}
+
+}  // namespace sushi

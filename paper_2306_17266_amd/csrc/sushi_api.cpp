@@ -15,6 +15,7 @@
 
 #include "../../include/sushi.h"
 #include "kernels.h"
+#include "logits.h"
 #include "model.h"
 #include "sched.h"
 #include "stream_kernel.h"
@@ -1785,6 +1786,127 @@ int sushi_infer_static(sushi_ctx *c, const sushi_subnet_cfg *cfg, const void *in
     s.last_hit_ratio = cp->hit_ratio;
     s.sum_hit_ratio += cp->hit_ratio;
     return SUSHI_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The checks that the operators on logits share: the rows, the workspace.
+int check_rows(sushi_ctx *c, const char *op, const sushi_logits *in, const void *ws, size_t ws_bytes, LogitRows *out) {
+    const std::string name(op);
+    if (c->device < 0) return fail(c, SUSHI_ESTATE, name + ": host-only context");
+    if (!in) return fail(c, SUSHI_EINVAL, name + ": null argument");
+    if (in->dtype != SUSHI_FP32 && in->dtype != SUSHI_BF16) return fail(c, SUSHI_EINVAL, name + ": unknown dtype");
+    if (in->rows < 0 || in->classes < 1 || in->classes > SUSHI_MAX_CLASSES || in->row_stride < in->classes || in->row_stride > (1ll << 40))
+        return fail(c, SUSHI_EINVAL, name + ": bad shape");
+    *out = LogitRows{in->data, (long)in->row_stride, in->rows, in->classes, in->dtype == SUSHI_BF16};
+    if (in->rows == 0) return SUSHI_OK;
+    if (!in->data || reinterpret_cast<uintptr_t>(in->data) % (out->bf16 ? 2 : 4)) return fail(c, SUSHI_EINVAL, name + ": logits are null or not aligned");
+    if (!ws || ws_bytes < logits_workspace_bytes(in->rows, in->classes) || reinterpret_cast<uintptr_t>(ws) % 16)
+        return fail(c, SUSHI_EINVAL, name + ": the workspace is too small or not aligned");
+    return SUSHI_OK;
+}
+
+// Pointers to 32-bit elements: given (null is allowed for optional ones) and aligned.
+bool words(std::initializer_list<const void *> needed, std::initializer_list<const void *> optional) {
+    for (const void *p : needed)
+        if (!p || reinterpret_cast<uintptr_t>(p) % 4) return false;
+    for (const void *p : optional)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
+}
+
+// Bytes from the first logit of the first row to the last of the last.
+size_t extent(const LogitRows &in, long stride) { return ((size_t)(in.rows - 1) * stride + in.n) * (in.bf16 ? 2 : 4); }
+
+// Runs an operator's launches on the context's stream, between events if timing is on.
+template <typename F>
+int run_operator(sushi_ctx *c, int kc, double bytes, double flops, F launch) {
+    hipError_t e;
+    if ((e = hipSetDevice(c->device)) != hipSuccess) return hip_fail(c, e, "hipSetDevice");
+    c->stream_dirty = true;
+    sushi_ctx::Pending pend{};
+    if (c->timing) {
+        if ((e = get_event(c, &pend.a)) != hipSuccess || (e = get_event(c, &pend.b)) != hipSuccess ||
+            (e = hipEventRecord(pend.a, c->stream)) != hipSuccess)
+            return hip_fail(c, e, "kernel timing");
+    }
+    if ((e = launch(c->stream)) != hipSuccess) return hip_fail(c, e, "kernel launch");
+    if (c->timing) {
+        if ((e = hipEventRecord(pend.b, c->stream)) != hipSuccess) return hip_fail(c, e, "kernel timing");
+        pend.kc = kc, pend.bytes = bytes, pend.flops = flops;
+        c->pending.push_back(pend);
+        if (c->pending.size() >= 4096 && (e = drain_timing(c)) != hipSuccess) return hip_fail(c, e, "kernel timing");
+    }
+    return SUSHI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sushi_logits_workspace(int32_t rows, int32_t classes, size_t *n_bytes) {
+    if (!n_bytes || rows < 0 || classes < 1 || classes > SUSHI_MAX_CLASSES) return SUSHI_EINVAL;
+    *n_bytes = std::max<size_t>(logits_workspace_bytes(rows, classes), 16);
+    return SUSHI_OK;
+}
+
+int sushi_sample(sushi_ctx *c, const sushi_logits *logits, const sushi_sampling *sampling, const float *uniform, int32_t *classes,
+                 float *log_prob, void *ws, size_t ws_bytes) {
+    if (!c) return SUSHI_EINVAL;
+    SampleArgs a{};
+    int rc = check_rows(c, "sample", logits, ws, ws_bytes, &a.in);
+    if (rc || a.in.rows == 0) return rc;
+    const sushi_sampling s = sampling ? *sampling : sushi_sampling{};
+    if (!words({uniform, classes}, {log_prob, s.temperature, s.top_k, s.top_p, s.min_p}))
+        return fail(c, SUSHI_EINVAL, "sample: a pointer is null or not aligned");
+    a.uniform = uniform, a.temperature = s.temperature, a.top_k = s.top_k, a.top_p = s.top_p, a.min_p = s.min_p;
+    a.classes = classes, a.log_prob = log_prob;
+    const double n = (double)a.in.rows * a.in.n;
+    return run_operator(c, KC_SAMPLE, n * (a.in.bf16 ? 2 : 4) + 12.0 * a.in.rows, 4.0 * n,
+                        [&](hipStream_t st) { return launch_sample(a, ws, st); });
+}
+
+int sushi_top_logits(sushi_ctx *c, const sushi_logits *logits, int k, float temperature, float *values, int32_t *classes, float *rest,
+                     void *ws, size_t ws_bytes) {
+    if (!c) return SUSHI_EINVAL;
+    TopArgs a{};
+    int rc = check_rows(c, "top_logits", logits, ws, ws_bytes, &a.in);
+    if (rc) return rc;
+    if (k < 1 || k > SUSHI_MAX_TOP || k > a.in.n) return fail(c, SUSHI_EINVAL, "top_logits: k is outside 1 .. min(classes, SUSHI_MAX_TOP)");
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return fail(c, SUSHI_EINVAL, "top_logits: the temperature is not positive and finite");
+    if (a.in.rows == 0) return SUSHI_OK;
+    if (!words({values, classes}, {rest})) return fail(c, SUSHI_EINVAL, "top_logits: a pointer is null or not aligned");
+    a.k = k, a.temperature = temperature, a.values = values, a.classes = classes, a.rest = rest;
+    const double n = (double)a.in.rows * a.in.n;
+    return run_operator(c, KC_TOP_LOGITS, n * (a.in.bf16 ? 2 : 4) + (8.0 * k + 4.0) * a.in.rows, 4.0 * n,
+                        [&](hipStream_t st) { return launch_top_logits(a, ws, st); });
+}
+
+int sushi_distill(sushi_ctx *c, const sushi_logits *student, const sushi_teacher *t, float temperature, const float *weight, float *loss,
+                  void *grad, int64_t grad_stride, void *ws, size_t ws_bytes) {
+    if (!c) return SUSHI_EINVAL;
+    DistillArgs a{};
+    int rc = check_rows(c, "distill", student, ws, ws_bytes, &a.in);
+    if (rc) return rc;
+    if (!t || t->k < 1 || t->k > SUSHI_MAX_TOP) return fail(c, SUSHI_EINVAL, "distill: the teacher's list is null or k outside 1 .. SUSHI_MAX_TOP");
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return fail(c, SUSHI_EINVAL, "distill: the temperature is not positive and finite");
+    if (grad && (grad_stride < a.in.n || grad_stride > (1ll << 40))) return fail(c, SUSHI_EINVAL, "distill: bad grad_stride");
+    if (a.in.rows == 0) return SUSHI_OK;
+    if (!words({t->values, t->classes}, {t->rest, weight, loss}) || reinterpret_cast<uintptr_t>(grad) % (a.in.bf16 ? 2 : 4))
+        return fail(c, SUSHI_EINVAL, "distill: a pointer is null or not aligned");
+    if (!loss && !grad) return fail(c, SUSHI_EINVAL, "distill: neither loss nor gradient is asked for");
+    if (grad && (grad != a.in.x || (a.in.rows > 1 && grad_stride != a.in.stride))) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.in.x), g = reinterpret_cast<uintptr_t>(grad);
+        if (x < g + extent(a.in, grad_stride) && g < x + extent(a.in, a.in.stride))
+            return fail(c, SUSHI_EINVAL, "distill: the gradient overlaps the logits without being in their place");
+    }
+    a.values = t->values, a.classes = t->classes, a.rest = t->rest, a.weight = weight, a.k = t->k, a.temperature = temperature;
+    a.loss = loss, a.grad = grad, a.grad_stride = grad_stride;
+    const double n = (double)a.in.rows * a.in.n;
+    return run_operator(c, KC_DISTILL, n * (a.in.bf16 ? 2 : 4) * (grad ? 2 : 1) + (8.0 * a.k + 4.0) * a.in.rows, (grad ? 6.0 : 4.0) * n,
+                        [&](hipStream_t st) { return launch_distill(a, ws, st); });
 }
 
 int sushi_sched_init(sushi_ctx *c, const sushi_sched_desc *d) {
