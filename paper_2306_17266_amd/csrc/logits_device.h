@@ -47,7 +47,7 @@ struct Weight {
     double best, scale;  // maximum; log2(e) / T
     bool infinite;
     __device__ __forceinline__ Weight(float m, double inv_t) : best(m), scale(inv_t * 1.4426950408889634074), infinite(m == INFINITY) {}
-    __device__ __forceinline__ double log2_of(float z) const {  // <= 0, or NaN for what has no weight
+    __device__ __forceinline__ double log2_of(float z) const {  // <= 0, -inf or NaN for what has no weight
         if (infinite) return z == INFINITY ? 0.0 : -INFINITY;
         return ((double)z - best) * scale;
     }
@@ -71,6 +71,33 @@ __device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(T)]) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     else
         return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+
+// Element e of a piece, e not known to the compiler (loops that run seldom stay small).
+template <typename T>
+__device__ __forceinline__ float element(uint4 r, int e) {
+    const int w = sizeof(T) == 4 ? e : e >> 1;
+    const uint32_t a = r.x, b = r.y, c = r.z, d = r.w;  // (a choice between the members themselves would be one between addresses)
+    const uint32_t lo = w & 1 ? b : a, hi = w & 1 ? d : c, u = w & 2 ? hi : lo;
+    if (sizeof(T) == 4) return __uint_as_float(u);
+    return __uint_as_float(e & 1 ? u & 0xFFFF0000u : u << 16);
+}
+
+// f(logit, index) for the elements of a piece that are at least z_low.
+template <typename T, typename F>
+__device__ __forceinline__ void from_piece(uint4 r, int j, float z_low, F f) {
+    float v[16 / sizeof(T)];
+    unpack<T>(r, v);
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) some |= v[e] >= z_low;
+    if (some) {
+#pragma unroll 1
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+            const float z = element<T>(r, e);
+            if (z >= z_low) f(z, j + e);
+        }
+    }
 }
 
 // One row, or a part of it, as a workgroup reads it: in pieces of 16 bytes at 16-byte addresses (the first and the last may be partly outside the
@@ -124,15 +151,99 @@ struct Row {
     __device__ __forceinline__ void each(F f) const {
         for (int i = 0; i < rounds; ++i) piece(i, f);
     }
+    // f(logit, index) for the elements that are at least z_low, few of them
+    template <typename F>
+    __device__ __forceinline__ void each_from(float z_low, F f) const {
+        for (int i = 0; i < rounds; ++i) from_piece<T>(load(i), index(i), z_low, f);
+    }
+};
+
+// p or q, by value (a conditional assignment of the whole piece may become a choice between two addresses, and the pieces go to memory).
+__device__ __forceinline__ uint4 choose(bool first, uint4 p, uint4 q) {
+    const uint32_t m = 0u - (uint32_t)first;
+    return make_uint4((p.x & m) | (q.x & ~m), (p.y & m) | (q.y & ~m), (p.z & m) | (q.z & ~m), (p.w & m) | (q.w & ~m));
+}
+
+// The same row, or part, in registers: at most N pieces a lane.
+template <typename T, int N>
+struct HeldRow : Row<T> {
+    using Row<T>::PER;
+    uint4 raw[N];
+
+    __device__ __forceinline__ HeldRow(const LogitRows &in, long row, int wave, int waves, int lane, int from = 0, int most = 0x7FFFFFFF)
+        : Row<T>(in, row, wave, waves, lane, from, most) {
+        // whole pieces first, all in flight together; then the row's ends
+        const int ends = (this->n + this->lead - 1) / PER;  // the last piece
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int j = this->index(i);
+            constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+            raw[i] = make_uint4(none, none, none, none);
+            if (i < this->rounds && j >= 0 && j + PER <= this->n) raw[i] = *reinterpret_cast<const uint4 *>(this->x + j);
+        }
+        if (this->first == 0 && this->lead > 0) raw[0] = this->load(0);
+        const int i_end = (ends - this->first) >> 6;
+        if (((ends - this->first) & 63) == 0 && i_end >= 0 && i_end < this->rounds && this->index(i_end) + PER > this->n) {
+            const uint4 r = this->load(i_end);
+#pragma unroll
+            for (int i = 0; i < N; ++i) raw[i] = choose(i == i_end, r, raw[i]);
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < this->rounds) {
+                float v[PER];
+                unpack<T>(raw[i], v);
+                const int j = this->index(i);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) f(v[e], j + e);
+            }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each_from(float z_low, F f) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < this->rounds) from_piece<T>(raw[i], this->index(i), z_low, f);
+    }
 };
 
 // ------------------------------------------------------------------ sums over a wave and a workgroup (the same in every run)
 
+// A value of 4 or 8 bytes from the lane that the pattern names; `other` where there is none or the row is masked out.
+template <int PATTERN, int ROWS, typename V>
+__device__ __forceinline__ V from_lane(V other, V v) {
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other), __builtin_bit_cast(int, v), PATTERN, ROWS, 0xF, false));
+    } else {
+        const int2 o = __builtin_bit_cast(int2, other), a = __builtin_bit_cast(int2, v);
+        int2 r;
+        r.x = __builtin_amdgcn_update_dpp(o.x, a.x, PATTERN, ROWS, 0xF, false);
+        r.y = __builtin_amdgcn_update_dpp(o.y, a.y, PATTERN, ROWS, 0xF, false);
+        return __builtin_bit_cast(V, r);
+    }
+}
+template <typename V>
+__device__ __forceinline__ V read_lane(V v, int lane) {
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        const int2 a = __builtin_bit_cast(int2, v);
+        int2 r;
+        r.x = __builtin_amdgcn_readlane(a.x, lane), r.y = __builtin_amdgcn_readlane(a.y, lane);
+        return __builtin_bit_cast(V, r);
+    }
+}
+
+// f over all lanes of the wave: within rows of 16 by exchanges, then over the four rows.
 template <typename V, typename F>
 __device__ __forceinline__ V wave_all(V v, F f) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = f(v, __shfl_xor(v, d));
-    return v;
+    v = f(v, from_lane<0xB1, 0xF>(v, v));   // neighbours
+    v = f(v, from_lane<0x4E, 0xF>(v, v));   // pairs of four
+    v = f(v, from_lane<0x141, 0xF>(v, v));  // mirrored halves of a row
+    v = f(v, from_lane<0x140, 0xF>(v, v));  // mirrored rows
+    return f(f(read_lane(v, 0), read_lane(v, 16)), f(read_lane(v, 32), read_lane(v, 48)));
 }
 template <typename V>
 __device__ __forceinline__ V wave_sum(V v) {
@@ -140,12 +251,13 @@ __device__ __forceinline__ V wave_sum(V v) {
 }
 // Sum over this lane and those before it.
 template <typename V>
-__device__ __forceinline__ V wave_scan(V v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const V u = __shfl_up(v, d);
-        v += lane >= d ? u : V(0);
-    }
+__device__ __forceinline__ V wave_scan(V v) {
+    v += from_lane<0x111, 0xF>(V(0), v);  // the lane 1, 2, 4, 8 before, within the row
+    v += from_lane<0x112, 0xF>(V(0), v);
+    v += from_lane<0x114, 0xF>(V(0), v);
+    v += from_lane<0x118, 0xF>(V(0), v);
+    v += from_lane<0x142, 0xA>(V(0), v);  // last lane of the row before, to rows 1 and 3
+    v += from_lane<0x143, 0xC>(V(0), v);  // lane 31, to rows 2 and 3
     return v;
 }
 
