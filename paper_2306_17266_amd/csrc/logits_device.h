@@ -190,16 +190,22 @@ struct HeldRow : Row<T> {
         }
     }
     template <typename F>
-    __device__ __forceinline__ void each(F f) const {
+    __device__ __forceinline__ void each_piece(F f) const {  // f(logits, index of the first)
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < this->rounds) {
                 float v[PER];
                 unpack<T>(raw[i], v);
-                const int j = this->index(i);
-#pragma unroll
-                for (int e = 0; e < PER; ++e) f(v[e], j + e);
+                f(v, this->index(i));
+                __builtin_amdgcn_sched_barrier(0);  // (one piece after the other: mixed, they take registers that spill)
             }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        each_piece([&](const float(&v)[PER], int j) {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) f(v[e], j + e);
+        });
     }
     template <typename F>
     __device__ __forceinline__ void each_from(float z_low, F f) const {
