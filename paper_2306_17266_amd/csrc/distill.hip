@@ -62,35 +62,40 @@ __device__ __forceinline__ bool entry_counts(const int *list, int i, int low, in
     return true;
 }
 
-// Marks of a piece whose first element is at bit b (a multiple of its length).
-template <typename T>
-__device__ __forceinline__ uint32_t piece_marks(const uint32_t *bits, int b) {
-    return bits[b >> 5] >> (b & 31);
-}
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }  // (NaN if one is)
 
-__device__ __forceinline__ float larger(float x, float y) { return x != x || y != y ? NAN : fmaxf(x, y); }
-
-// The maximum of a row or part, NaN if there is one, and its share of R at a maximum.
-template <int THREADS, typename R>
-__device__ __forceinline__ float largest(const R &row, float *part) {
+// The maximum of this thread's logits, NaN if there is one.
+template <typename R>
+__device__ __forceinline__ float own_largest(const R &row) {
     float m = -INFINITY;
-    bool nan = false;
-    row.each([&](float z, int) { m = fmaxf(m, z), nan |= z != z; });
-    return block_all<THREADS>(nan ? NAN : m, part, larger);
+    row.each([&](float z, int) { m = larger(m, z); });
+    return m;
 }
-template <typename T, typename R>
-__device__ __forceinline__ double sum_unlisted(const R &row, const Weight &weight, const uint32_t *bits, int origin) {
-    double rest = 0.0;
-    row.each_piece([&](const float(&v)[R::PER], int j) {
-        const uint32_t marks = piece_marks<T>(bits, j - origin);
+
+// Takes the listed classes out of a row in registers (they read as -inf): their terms are summed apart.  origin: index of bit 0.
+template <typename T, int N>
+__device__ __forceinline__ void leave_unlisted(HeldRow<T, N> &row, const uint32_t *bits, int origin) {
+    constexpr int PER = HeldRow<T, N>::PER;
 #pragma unroll
-        for (int e = 0; e < R::PER; ++e) {
-            const double w = exp2_64<7>(weight.log2_of(v[e]));
-            rest += marks >> e & 1 ? 0.0 : w;
+    for (int i = 0; i < N; ++i) {
+        const int b = row.index(i) - origin;  // (a multiple of PER)
+        const uint32_t marks = i < row.rounds ? bits[b >> 5] >> (b & 31) & ((1u << PER) - 1) : 0;
+        if (marks) {
+            float v[PER];
+            unpack<T>(row.raw[i], v);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) v[e] = marks >> e & 1 ? -INFINITY : v[e];
+            row.raw[i] = pack<T>(v);
         }
-    });
-    return rest;
+    }
 }
+
+// Weights of listed classes, one at a time.
+struct Terms : Weight {
+    bool infinite;
+    __device__ __forceinline__ Terms(float m, double inv_t) : Weight(m == INFINITY ? 0.0f : m, inv_t), infinite(m == INFINITY) {}
+    __device__ __forceinline__ double log2_of(float z) const { return Weight::log2_of(infinite ? as_infinite(z) : z); }
+};
 
 // This thread's entries of a row's list.
 template <int OWN>
@@ -98,121 +103,160 @@ struct Entries {
     bool counts[OWN];
     float t[OWN], z[OWN];
 };
-
-// The row's loss (written) and what its gradient needs, from its maximum m and R, which every thread has.
 template <typename T, int THREADS, int OWN>
-__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, float m, double rest, const Entries<OWN> &own, float *part_f, double (*part_d)[THREADS / 64]) {
-    float tm = -INFINITY;
-#pragma unroll
-    for (int o = 0; o < OWN; ++o) tm = larger(tm, own.t[o]);
-    tm = block_all<THREADS>(tm, part_f, larger);
-    const double inv_t = 1.0 / (double)a.temperature;
-    const Weight student(m, inv_t), teacher(tm, inv_t);
-    double sum = 0.0, list_sum = 0.0;
-#pragma unroll
-    for (int o = 0; o < OWN; ++o)
-        if (own.counts[o]) sum += exp2_64<11>(student.log2_of(own.z[o])), list_sum += exp2_64<11>(teacher.log2_of(own.t[o]));
-    sum = wave_sum(sum), list_sum = wave_sum(list_sum);
-    if ((threadIdx.x & 63) == 0) part_d[0][threadIdx.x >> 6] = sum, part_d[1][threadIdx.x >> 6] = list_sum;
-    __syncthreads();
-    sum = rest, list_sum = 0.0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += part_d[0][w], list_sum += part_d[1][w];
-    const bool nan = m != m || tm != tm;
-    double mass = a.rest ? (double)a.rest[r] : 0.0;  // outside the list
-    mass = mass < 0.0 ? 0.0 : mass > 1.0 ? 1.0 : mass;
-    const bool empty = !nan && (m == -INFINITY || tm == -INFINITY);
-    if (a.loss) {
-        double loss = 0.0;
-        const double log_sum = log(sum), log_list = log1p(-mass) - log(list_sum);
-#pragma unroll
-        for (int o = 0; o < OWN; ++o)
-            if (own.counts[o]) {
-                const double log_p = teacher.log2_of(own.t[o]) * LN2 + log_list;
-                const double p = exp(log_p);
-                if (p != 0.0) loss += p * (log_p - (student.log2_of(own.z[o]) * LN2 - log_sum));
-            }
-        loss = block_sum<THREADS>(loss, part_d[2]);
-        if (threadIdx.x == 0) {
-            if (mass != 0.0) loss += mass * (log(mass) - (log(rest) - log_sum));
-            a.loss[r] = empty ? 0.0f : nan ? NAN : (float)loss;
-        }
-    }
-    const float w = empty ? 0.0f : a.weight ? a.weight[r] : 1.0f;
-    const double share = mass == 0.0 ? 1.0 / sum : rest > 0.0 ? 1.0 / sum - mass / rest : 0.0;
-    return RowSums{nan ? NAN : 1.0 / sum, (1.0 - mass) / list_sum, nan ? NAN : w * inv_t * share, m, tm, (float)(w * inv_t), 0.0f};
-}
-
-// Gradient of a listed class.
-__device__ __forceinline__ float list_gradient(const RowSums &s, double inv_t, float z, float t) {
-    const double e = exp2_64<11>(Weight(s.best, inv_t).log2_of(z)), p = exp2_64<11>(Weight(s.list_best, inv_t).log2_of(t)) * s.list_scale;
-    return (float)((e * s.inv_sum - p) * (double)s.weight);
-}
-
-// Gradient of every class of a row or part as if it were not listed.  The weights have 32 bits here: what a gradient of 32 bits is left
-// with is the rounding of the exponent, 2^-24 of it thrice.
-template <typename T, typename R>
-__device__ __forceinline__ void write_gradient(const DistillArgs &a, const R &row, T *grad, const RowSums &s) {
-    constexpr int PER = R::PER;
-    const double inv_t = 1.0 / (double)a.temperature;
-    const bool together = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0;
-    const bool zero = s.weight == 0.0f, infinite = s.best == INFINITY;
-    const float scale = (float)(inv_t * 1.4426950408889634074), out = zero ? 0.0f : (float)s.rest_scale;
-    row.each_piece([&](const float(&v)[PER], int j) {
-        float g[PER];
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const float w = infinite ? (v[e] == INFINITY ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f((v[e] - s.best) * scale);
-            g[e] = zero ? 0.0f : w * out;
-        }
-        if (together && j >= 0 && j + PER <= a.in.n) {
-            *reinterpret_cast<uint4 *>(grad + j) = pack<T>(g);
-        } else {
-#pragma unroll
-            for (int e = 0; e < PER; ++e)
-                if (j + e >= 0 && j + e < a.in.n) st1(grad + j + e, g[e]);
-        }
-    });
-}
-
-template <typename T>
-__device__ __forceinline__ float logit(const DistillArgs &a, long r, int c) {
-    return ld1(static_cast<const T *>(a.in.x) + r * a.in.stride + c);
-}
-
-// ------------------------------------------------------------------ a row in the registers of a workgroup
-
-template <typename T, int N, int THREADS>
-__global__ __launch_bounds__(THREADS, 4) void distill_held_kernel(DistillArgs a, int row0) {
-    constexpr int SPAN = N * THREADS * 16 / (int)sizeof(T), OWN = (LOGITS_MAX_TOP + THREADS - 1) / THREADS;
-    __shared__ uint32_t bits[SPAN / 32];
-    __shared__ int list[LOGITS_MAX_TOP];
-    __shared__ int twice;
-    __shared__ float part_f[2][THREADS / 64];
-    __shared__ double part_d[4][THREADS / 64];
-    const long r = (long)row0 + blockIdx.x;
-    const HeldRow<T, N> row(a.in, r, threadIdx.x >> 6, THREADS / 64, threadIdx.x & 63);
-    mark_list<THREADS>(a, r, 0, a.in.n, -row.lead, SPAN - 1, bits, list, &twice);
+__device__ __forceinline__ Entries<OWN> read_entries(const DistillArgs &a, long r, const int *list, int twice) {
     Entries<OWN> own;
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
         const int i = o * THREADS + threadIdx.x;
         own.counts[o] = i < a.k && entry_counts(list, i, 0, a.in.n, twice);
         own.t[o] = own.counts[o] ? a.values[r * a.k + i] : -INFINITY;
-        own.z[o] = own.counts[o] ? logit<T>(a, r, list[i]) : -INFINITY;
+        own.z[o] = own.counts[o] ? ld1(static_cast<const T *>(a.in.x) + r * a.in.stride + list[i]) : -INFINITY;
     }
-    const float m = largest<THREADS>(row, part_f[0]);
+    return own;
+}
+
+// The maxima of the row (from each thread's own) and of its list.
+template <int THREADS, int OWN>
+__device__ __forceinline__ void maxima(float &m, float &tm, const Entries<OWN> &own, float (*part)[THREADS / 64]) {
+    tm = -INFINITY;
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) tm = larger(tm, own.t[o]);
+    m = wave_all(m, larger), tm = wave_all(tm, larger);
+    if ((threadIdx.x & 63) == 0) part[0][threadIdx.x >> 6] = m, part[1][threadIdx.x >> 6] = tm;
+    __syncthreads();
+    m = across_waves<THREADS / 64>(part[0], larger), tm = across_waves<THREADS / 64>(part[1], larger);
+}
+
+// The row's loss (written) and what its gradient needs, from the maxima and each thread's part of R.  Only the waves that have
+// entries compute with them.
+template <int THREADS, int OWN>
+__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, float m, float tm, double rest, const Entries<OWN> &own, double (*part)[THREADS / 64]) {
+    const int wave = threadIdx.x >> 6;
+    const bool entries = wave * 64 < a.k;
     const double inv_t = 1.0 / (double)a.temperature;
-    const double rest = block_sum<THREADS>(sum_unlisted<T>(row, Weight(m, inv_t), bits, -row.lead), part_d[3]);
-    const RowSums s = finish_row<T, THREADS>(a, r, m, rest, own, part_f[1], part_d);
+    const Terms student(m, inv_t), teacher(tm, inv_t);
+    double sum = 0.0, list_sum = 0.0;
+    if (entries) {
+#pragma unroll
+        for (int o = 0; o < OWN; ++o)
+            if (own.counts[o]) sum += exp2_64<11>(student.log2_of(own.z[o])), list_sum += exp2_64<11>(teacher.log2_of(own.t[o]));
+        sum = wave_sum(sum), list_sum = wave_sum(list_sum);
+    }
+    rest = wave_sum(rest);
+    if ((threadIdx.x & 63) == 0) part[0][wave] = rest, part[1][wave] = sum, part[2][wave] = list_sum;
+    __syncthreads();
+    rest = sum_across<THREADS / 64>(part[0]), sum = rest + sum_across<THREADS / 64>(part[1]), list_sum = sum_across<THREADS / 64>(part[2]);
+    const bool nan = m != m || tm != tm;
+    double mass = a.rest ? (double)a.rest[r] : 0.0;  // outside the list
+    mass = mass < 0.0 ? 0.0 : mass > 1.0 ? 1.0 : mass;
+    const bool empty = !nan && (m == -INFINITY || tm == -INFINITY);
+    if (a.loss) {
+        double loss = 0.0;
+        if (entries) {
+            const double log_sum = log(sum), log_list = log1p(-mass) - log(list_sum);
+#pragma unroll
+            for (int o = 0; o < OWN; ++o)
+                if (own.counts[o]) {
+                    const double log_p = teacher.log2_of(own.t[o]) * LN2 + log_list;
+                    const double p = exp2_64<11>(log_p * 1.4426950408889634074);
+                    // (p = 0 counts nothing; what makes log_p NaN shows in the maxima or in the mass)
+                    if (p != 0.0) loss += p * (log_p - (student.log2_of(own.z[o]) * LN2 - log_sum));
+                }
+            loss = wave_sum(loss);
+            if (wave == 0 && mass != 0.0) loss += mass * (log(mass) - (log(rest) - log_sum));
+        }
+        if (a.k > 64) {
+            if ((threadIdx.x & 63) == 0) part[3][wave] = loss;
+            __syncthreads();
+            loss = sum_across<THREADS / 64>(part[3]);
+        }
+        if (threadIdx.x == 0) a.loss[r] = empty ? 0.0f : nan ? NAN : (float)loss;
+    }
+    const float w = empty ? 0.0f : a.weight ? a.weight[r] : 1.0f;
+    const double inv_sum = 1.0 / sum, share = mass == 0.0 ? inv_sum : rest > 0.0 ? inv_sum - mass / rest : 0.0;
+    return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan ? NAN : w * inv_t * share, m, tm, (float)(w * inv_t), 0.0f};
+}
+
+// Gradient of a listed class.
+__device__ __forceinline__ float list_gradient(const RowSums &s, double inv_t, float z, float t) {
+    const double e = exp2_64<11>(Terms(s.best, inv_t).log2_of(z)), p = exp2_64<11>(Terms(s.list_best, inv_t).log2_of(t)) * s.list_scale;
+    return (float)((e * s.inv_sum - p) * (double)s.weight);
+}
+
+// Gradients of the others.  Weights have 32 bits here: what a gradient of 32 bits is left with is the rounding of the exponent, 2^-24
+// of it thrice.
+struct GradientOf {
+    float best, scale, out;
+    __device__ __forceinline__ GradientOf(const RowSums &s, double inv_t)
+        : best(s.best == INFINITY || s.weight == 0.0f ? 0.0f : s.best), scale((float)(1.4426950408889634074 * inv_t)),
+          out(s.weight == 0.0f ? 0.0f : (float)s.rest_scale) {}
+    __device__ __forceinline__ float of(float z) const { return __builtin_amdgcn_exp2f((z - best) * scale) * out; }
+};
+
+// The elements of piece r (first index j) that are in the row, one by one.
+template <typename T>
+__device__ __forceinline__ void store_elements(T *grad, int n, int j, uint4 r) {
+#pragma unroll 1
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e)
+        if (j + e >= 0 && j + e < n) st1(grad + j + e, element<T>(r, e));
+}
+
+// ------------------------------------------------------------------ a row in the registers of a workgroup
+
+// For gradients whose rows lie to 16 bytes as those of the logits do.  The logits stay in registers as they came, and their weights are
+// computed again for the gradient: with 80 registers three workgroups of 512 share a compute unit, and one loads or stores while
+// another computes (kept weights need 128: 199 us against 154 at 4096 x 32000 bf16).
+template <typename T, int N, int THREADS>
+__global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a, int row0) {
+    constexpr int PER = 16 / sizeof(T), SPAN = N * THREADS * PER, OWN = (LOGITS_MAX_TOP + THREADS - 1) / THREADS;
+    __shared__ uint32_t bits[SPAN / 32];
+    __shared__ int list[LOGITS_MAX_TOP];
+    __shared__ int twice;
+    __shared__ float part_f[2][THREADS / 64];
+    __shared__ double part_d[4][THREADS / 64];
+    const long r = (long)row0 + blockIdx.x;
+    HeldRow<T, N> row(a.in, r, threadIdx.x >> 6, THREADS / 64, threadIdx.x & 63);
+    mark_list<THREADS>(a, r, 0, a.in.n, -row.lead, SPAN - 1, bits, list, &twice);
+    const Entries<OWN> own = read_entries<T, THREADS, OWN>(a, r, list, twice);
+    float m = own_largest(row), tm;
+    maxima<THREADS>(m, tm, own, part_f);
+    const double inv_t = 1.0 / (double)a.temperature;
+    if (m == INFINITY) row.only_infinite();
+    leave_unlisted(row, bits, -row.lead);
+    const Weight weight(m == INFINITY ? 0.0f : m, inv_t);
+    double rest = 0.0;
+    row.each([&](float z, int) { rest += exp2_64<6>(weight.log2_of(z)); });
+    const RowSums s = finish_row<THREADS>(a, r, m, tm, rest, own, part_d);
     if (!a.grad) return;
     // (the gradient may take the logits' place: every thread has passed a barrier since its logits were read)
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
-    write_gradient<T>(a, row, grad, s);
+    const bool zero = s.weight == 0.0f;
+    if (zero) row.none();
+    const GradientOf gradient(s, inv_t);
+    T *piece = grad + row.index(0);
+    uint4 start = row.raw[0], end = row.raw[0];
+    const int i_end = row.partial_end();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < row.rounds) {
+            float v[PER];
+            unpack<T>(row.raw[i], v);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) v[e] = gradient.of(v[e]);
+            const uint4 g = pack<T>(v);
+            const int j = row.index(i);
+            if (j >= 0 && j + PER <= a.in.n) *reinterpret_cast<uint4 *>(piece + i * 64 * PER) = g;
+            if (i == 0) start = g;
+            end = choose(i == i_end, g, end);
+            apart();
+        }
+    if (row.index(0) < 0 && row.index(0) + PER > 0) store_elements(grad, a.in.n, row.index(0), start);
+    if (i_end >= 0) store_elements(grad, a.in.n, row.index(i_end), end);
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < OWN; ++o)
-        if (own.counts[o]) st1(grad + list[o * THREADS + threadIdx.x], s.weight == 0.0f ? 0.0f : list_gradient(s, inv_t, own.z[o], own.t[o]));
+        if (own.counts[o]) st1(grad + list[o * THREADS + threadIdx.x], zero ? 0.0f : list_gradient(s, inv_t, own.z[o], own.t[o]));
 }
 
 // ------------------------------------------------------------------ a row in parts
@@ -229,11 +273,16 @@ __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, in
     __shared__ double part_d[THREADS / 64];
     const long r = (long)row0 + blockIdx.x / parts;
     const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const HeldRow<T, PART_PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
+    HeldRow<T, PART_PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
     const int origin = first_index(part, PER, row.lead);
     mark_list<THREADS>(a, r, max(origin, 0), min(origin + SPAN, a.in.n), origin, SPAN - 1, bits, list, &twice);
-    const float m = largest<THREADS>(row, part_f);
-    const double rest = block_sum<THREADS>(sum_unlisted<T>(row, Weight(m, 1.0 / (double)a.temperature), bits, origin), part_d);
+    const float m = block_all<THREADS>(own_largest(row), part_f, larger);
+    if (m == INFINITY) row.only_infinite();
+    leave_unlisted(row, bits, origin);
+    const Weight weight(m == INFINITY ? 0.0f : m, 1.0 / (double)a.temperature);
+    double rest = 0.0;
+    row.each([&](float z, int) { rest += exp2_64<6>(weight.log2_of(z)); });
+    rest = block_sum<THREADS>(rest, part_d);
     if (threadIdx.x == 0) out[blockIdx.x] = PartSums{rest, m, 0.0f};
 }
 
@@ -251,23 +300,15 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     while ((int)mask + 1 < n && mask + 1 < LIST_BITS) mask = mask * 2 + 1;
     mark_list<THREADS>(a, r, 0, n, 0, mask, bits, list, &twice);
     in += (long)blockIdx.x * parts;
-    float m = -INFINITY;
+    const Entries<OWN> own = read_entries<T, THREADS, OWN>(a, r, list, twice);
+    float m = -INFINITY, tm;
     for (int p = threadIdx.x; p < parts; p += THREADS) m = larger(m, in[p].best);
-    Entries<OWN> own;
-#pragma unroll
-    for (int o = 0; o < OWN; ++o) {
-        const int i = o * THREADS + threadIdx.x;
-        own.counts[o] = i < a.k && entry_counts(list, i, 0, n, twice);
-        own.t[o] = own.counts[o] ? a.values[r * a.k + i] : -INFINITY;
-        own.z[o] = own.counts[o] ? logit<T>(a, r, list[i]) : -INFINITY;
-    }
-    m = block_all<THREADS>(m, part_f[0], larger);
-    const Weight student(m, 1.0 / (double)a.temperature);
+    maxima<THREADS>(m, tm, own, part_f);
+    const Terms student(m, 1.0 / (double)a.temperature);
     double rest = 0.0;
     for (int p = threadIdx.x; p < parts; p += THREADS)
         if (in[p].rest != 0.0) rest += in[p].rest * exp2_64<11>(student.log2_of(in[p].best));
-    rest = block_sum<THREADS>(rest, part_d[3]);
-    const RowSums s = finish_row<T, THREADS>(a, r, m, rest, own, part_f[1], part_d);
+    const RowSums s = finish_row<THREADS>(a, r, m, tm, rest, own, part_d);
     if (threadIdx.x == 0) out[blockIdx.x] = s;
 }
 
@@ -279,7 +320,7 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a, in
     __shared__ int twice;
     const long r = (long)row0 + blockIdx.x / parts;
     const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const HeldRow<T, PART_PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
+    Row<T> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
     const int origin = first_index(part, PER, row.lead), low = max(origin, 0), high = min(origin + SPAN, a.in.n);
     const RowSums s = in[blockIdx.x / parts];
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
@@ -292,10 +333,23 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a, in
         const int i = o * THREADS + threadIdx.x;
         counts[o] = i < a.k && entry_counts(list, i, low, high, twice);
         own[o] = 0.0f;
-        if (counts[o] && s.weight != 0.0f) own[o] = list_gradient(s, 1.0 / (double)a.temperature, logit<T>(a, r, list[i]), a.values[r * a.k + i]);
+        if (counts[o] && s.weight != 0.0f) own[o] = list_gradient(s, 1.0 / (double)a.temperature, ld1(row.x + list[i]), a.values[r * a.k + i]);
     }
     __syncthreads();
-    write_gradient<T>(a, row, grad, s);
+    if (s.best == INFINITY) row.only_infinite();
+    const bool together = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0, zero = s.weight == 0.0f;
+    const GradientOf gradient(s, 1.0 / (double)a.temperature);
+    for (int i = 0; i < row.rounds; ++i) {
+        float v[PER];
+        unpack<T>(row.load(i), v);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[e] = zero ? 0.0f : gradient.of(v[e]);
+        const int j = row.index(i);
+        if (together && j >= 0 && j + PER <= a.in.n)
+            *reinterpret_cast<uint4 *>(grad + j) = pack<T>(v);
+        else
+            store_elements(grad, a.in.n, j, pack<T>(v));
+    }
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < OWN; ++o)
@@ -306,7 +360,8 @@ template <typename T, int N, int HELD>
 hipError_t launch_held(const DistillArgs &a, hipStream_t s) {
     const long most = (1l << 31) / HELD;
     for (long first = 0; first < a.in.rows; first += most) {
-        distill_held_kernel<T, N, HELD><<<(int)std::min<long>(a.in.rows - first, most), HELD, 0, s>>>(a, (int)first);
+        const int n = (int)std::min<long>(a.in.rows - first, most);
+        distill_held_kernel<T, N, HELD><<<n, HELD, 0, s>>>(a, (int)first);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -320,10 +375,12 @@ template <typename T>
 hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
     constexpr int PER = 16 / sizeof(T);
     const int pieces = (a.in.n + 2 * PER - 2) / PER;  // (a row may start inside its first piece)
-    if (pieces <= 256) return launch_held<T, 1, 256>(a, s);
-    if (pieces <= 1024) return launch_held<T, 4, 256>(a, s);
-    if (pieces <= 4096) return launch_held<T, 8, 512>(a, s);
-    if (pieces <= 8192 && a.in.rows >= 256) return launch_held<T, 8, 1024>(a, s);
+    const bool together = !a.grad || ((reinterpret_cast<uintptr_t>(a.grad) - reinterpret_cast<uintptr_t>(a.in.x)) % 16 == 0 &&
+                                      (a.in.rows == 1 || (a.grad_stride - a.in.stride) * (long)sizeof(T) % 16 == 0));
+    if (together && pieces <= 256) return launch_held<T, 1, 256>(a, s);
+    if (together && pieces <= 1024) return launch_held<T, 4, 256>(a, s);
+    if (together && pieces <= 4096) return launch_held<T, 8, 512>(a, s);
+    if (together && pieces <= 8192 && a.in.rows >= 256) return launch_held<T, 8, 1024>(a, s);
     const int parts = logits_parts(a.in.n, a.in.bf16);
     const int most = rows_of_slice(a.in.rows, a.in.n);
     RowSums *rows = reinterpret_cast<RowSums *>(ws);

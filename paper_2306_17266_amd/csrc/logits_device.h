@@ -17,41 +17,41 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-// 2^t for t <= 0 in 64 bits: t = i + f with |f| <= 1/2, the power series of 2^f up to f^DEGREE (what is left out: 2e-14 of the
-// value at most with degree 11, 5e-9 with 7), and i into the exponent.  Below 2^-1022, for -inf and for NaN: zero.
-template <int DEGREE>
+// 2^t for t <= 0 in 64 bits: t = i + f with |f| <= 1/2, a polynomial for 2^f, and i into the exponent.  Below 2^-1022, for -inf
+// and for NaN: zero.  TERMS = 11: the power series, off by 2e-14 of the value at most.  TERMS = 6: for sums, off by 2e-9 at most; the
+// coefficients come from a least-squares fit of the relative error, reweighted until its largest values were level, with 1 at f = 0.
+template <int TERMS>
 __device__ __forceinline__ double exp2_64(double t) {
+    static_assert(TERMS == 6 || TERMS == 11, "one of the two polynomials");
     t = fmax(t, -1100.0);
     const double i = __builtin_rint(t), f = t - i;
-    // (ln 2)^n / n!
-    constexpr double c[12] = {1.0,
-                              6.931471805599453094e-01,
-                              2.402265069591007123e-01,
-                              5.550410866482157995e-02,
-                              9.618129107628477162e-03,
-                              1.333355814642844343e-03,
-                              1.540353039338160995e-04,
-                              1.525273380405984028e-05,
-                              1.321548679014430949e-06,
-                              1.017808600923969973e-07,
-                              7.054911620801123330e-09,
-                              4.445538271870811498e-10};
-    double p = c[DEGREE];
+    double p;
+    if constexpr (TERMS == 6) {
+        constexpr double c[6] = {0.6931472028559306, 0.24022647913391443, 0.05550332468951376, 0.009618437385012474, 0.0013398875357849087, 0.00015353355071142543};
+        p = c[5];
 #pragma unroll
-    for (int n = DEGREE - 1; n >= 0; --n) p = fma(p, f, c[n]);
-    return ldexp(p, (int)i);
+        for (int n = 4; n >= 0; --n) p = fma(p, f, c[n]);
+    } else {  // (ln 2)^n / n!
+        constexpr double c[11] = {6.931471805599453094e-01, 2.402265069591007123e-01, 5.550410866482157995e-02, 9.618129107628477162e-03,
+                                  1.333355814642844343e-03, 1.540353039338160995e-04, 1.525273380405984028e-05, 1.321548679014430949e-06,
+                                  1.017808600923969973e-07, 7.054911620801123330e-09, 4.445538271870811498e-10};
+        p = c[10];
+#pragma unroll
+        for (int n = 9; n >= 0; --n) p = fma(p, f, c[n]);
+    }
+    return ldexp(fma(p, f, 1.0), (int)i);
 }
 
-// Weights of a row's logits at a temperature.  With an infinite maximum the limit: the infinite ones share the row.
+// Weights of a row's logits at a temperature: 2^log2_of().  An infinite maximum is no case of its own here: its row is read as
+// Row::only_infinite() says.
 struct Weight {
     double best, scale;  // maximum; log2(e) / T
-    bool infinite;
-    __device__ __forceinline__ Weight(float m, double inv_t) : best(m), scale(inv_t * 1.4426950408889634074), infinite(m == INFINITY) {}
-    __device__ __forceinline__ double log2_of(float z) const {  // <= 0, -inf or NaN for what has no weight
-        if (infinite) return z == INFINITY ? 0.0 : -INFINITY;
-        return ((double)z - best) * scale;
-    }
+    __device__ __forceinline__ Weight(float m, double inv_t) : best(m), scale(inv_t * 1.4426950408889634074) {}
+    __device__ __forceinline__ double log2_of(float z) const { return ((double)z - best) * scale; }  // <= 0, or NaN for what has no weight
 };
+
+// Where the maximum is +inf the weights have a limit: the infinite logits share the row.  The same weights as those of zeros among -inf.
+__device__ __forceinline__ float as_infinite(float z) { return z == INFINITY ? 0.0f : -INFINITY; }
 
 // ------------------------------------------------------------------ a row
 
@@ -71,6 +71,15 @@ __device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(T)]) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     else
         return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 share_infinite(uint4 r) {
+    float v[16 / sizeof(T)];
+    unpack<T>(r, v);
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) v[e] = as_infinite(v[e]);
+    return pack<T>(v);
 }
 
 // Element e of a piece, e not known to the compiler (loops that run seldom stay small).
@@ -107,9 +116,11 @@ __device__ __forceinline__ void from_piece(uint4 r, int j, float z_low, F f) {
 template <typename T>
 struct Row {
     static constexpr int PER = 16 / sizeof(T);  // logits of a piece
+    static constexpr uint32_t NONE = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
     const T *x;
     int n, lead;        // logits; elements of the first piece before the row
     int first, rounds;  // this lane's first piece, and how many it has (64 apart)
+    bool infinite = false;
 
     // A part: `most` pieces, a multiple of 64 * waves, from piece `from` on.
     __device__ __forceinline__ Row(const LogitRows &in, long row, int wave, int waves, int lane, int from = 0, int most = 0x7FFFFFFF) {
@@ -121,11 +132,17 @@ struct Row {
         first = from + wave * rounds * 64 + lane;
     }
     __device__ __forceinline__ int index(int i) const { return (first + i * 64) * PER - lead; }  // of the piece's first element
+    // From here on the row reads as as_infinite() of its logits.
+    __device__ __forceinline__ void only_infinite() { infinite = true; }
     __device__ __forceinline__ uint4 load(int i) const {
+        uint4 r = load_plain(i);
+        if (infinite) r = share_infinite<T>(r);
+        return r;
+    }
+    __device__ __forceinline__ uint4 load_plain(int i) const {
         const int j = index(i);
         if (j >= 0 && j + PER <= n) return *reinterpret_cast<const uint4 *>(x + j);
-        constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
-        uint32_t w[4] = {none, none, none, none};
+        uint32_t w[4] = {NONE, NONE, NONE, NONE};
         if (j + PER > 0 && j < n) {
 #pragma unroll
             for (int e = 0; e < PER; ++e)
@@ -158,6 +175,9 @@ struct Row {
     }
 };
 
+// What stands on both sides is not mixed by the compiler: four logits at a time fill the pipelines, more of them take registers that spill.
+__device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
+
 // p or q, by value (a conditional assignment of the whole piece may become a choice between two addresses, and the pieces go to memory).
 __device__ __forceinline__ uint4 choose(bool first, uint4 p, uint4 q) {
     const uint32_t m = 0u - (uint32_t)first;
@@ -173,21 +193,33 @@ struct HeldRow : Row<T> {
     __device__ __forceinline__ HeldRow(const LogitRows &in, long row, int wave, int waves, int lane, int from = 0, int most = 0x7FFFFFFF)
         : Row<T>(in, row, wave, waves, lane, from, most) {
         // whole pieces first, all in flight together; then the row's ends
-        const int ends = (this->n + this->lead - 1) / PER;  // the last piece
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int j = this->index(i);
-            constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
-            raw[i] = make_uint4(none, none, none, none);
+            raw[i] = make_uint4(Row<T>::NONE, Row<T>::NONE, Row<T>::NONE, Row<T>::NONE);
             if (i < this->rounds && j >= 0 && j + PER <= this->n) raw[i] = *reinterpret_cast<const uint4 *>(this->x + j);
         }
         if (this->first == 0 && this->lead > 0) raw[0] = this->load(0);
-        const int i_end = (ends - this->first) >> 6;
-        if (((ends - this->first) & 63) == 0 && i_end >= 0 && i_end < this->rounds && this->index(i_end) + PER > this->n) {
+        const int i_end = partial_end();
+        if (i_end >= 0) {
             const uint4 r = this->load(i_end);
 #pragma unroll
             for (int i = 0; i < N; ++i) raw[i] = choose(i == i_end, r, raw[i]);
         }
+    }
+    // Round of this lane's piece that holds the row's last element, if it is partly outside the row; else -1.
+    __device__ __forceinline__ int partial_end() const {
+        const int d = (this->n + this->lead - 1) / PER - this->first;
+        const int i = d >> 6;
+        return (d & 63) == 0 && i >= 0 && i < this->rounds && this->index(i) + PER > this->n ? i : -1;
+    }
+    __device__ __forceinline__ void only_infinite() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = share_infinite<T>(raw[i]);
+    }
+    __device__ __forceinline__ void none() {  // all -inf
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = make_uint4(Row<T>::NONE, Row<T>::NONE, Row<T>::NONE, Row<T>::NONE);
     }
     template <typename F>
     __device__ __forceinline__ void each_piece(F f) const {  // f(logits, index of the first)
@@ -197,14 +229,17 @@ struct HeldRow : Row<T> {
                 float v[PER];
                 unpack<T>(raw[i], v);
                 f(v, this->index(i));
-                __builtin_amdgcn_sched_barrier(0);  // (one piece after the other: mixed, they take registers that spill)
+                apart();
             }
     }
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         each_piece([&](const float(&v)[PER], int j) {
 #pragma unroll
-            for (int e = 0; e < PER; ++e) f(v[e], j + e);
+            for (int e = 0; e < PER; ++e) {
+                f(v[e], j + e);
+                if (e % 4 == 3) apart();
+            }
         });
     }
     template <typename F>
@@ -267,17 +302,39 @@ __device__ __forceinline__ V wave_scan(V v) {
     return v;
 }
 
+// f over what the waves of a workgroup left in LDS: one read and exchanges within a row of lanes.
+template <int WAVES, typename V, typename F>
+__device__ __forceinline__ V over_lanes(V v, F f) {  // lanes w + i * WAVES hold the same value
+    static_assert(WAVES == 1 || WAVES == 2 || WAVES == 4 || WAVES == 8 || WAVES == 16, "a row of lanes");
+    if constexpr (WAVES >= 2) v = f(v, from_lane<0xB1, 0xF>(v, v));
+    if constexpr (WAVES >= 4) v = f(v, from_lane<0x4E, 0xF>(v, v));
+    if constexpr (WAVES >= 8) v = f(v, from_lane<0x141, 0xF>(v, v));
+    if constexpr (WAVES >= 16) v = f(v, from_lane<0x140, 0xF>(v, v));
+    return read_lane(v, 0);
+}
+template <int WAVES, typename V, typename F>
+__device__ __forceinline__ V across_waves(const V *part, F f) {
+    return over_lanes<WAVES>(part[threadIdx.x & (WAVES - 1)], f);
+}
+template <int WAVES, typename V>
+__device__ __forceinline__ V sum_across(const V *part) {
+    return across_waves<WAVES>(part, [](V a, V b) { return a + b; });
+}
+// Sum of what the waves before this one left.
+template <int WAVES, typename V>
+__device__ __forceinline__ V sum_before(const V *part) {
+    const int w = threadIdx.x & (WAVES - 1);
+    const V masked = w < (int)(threadIdx.x >> 6) ? part[w] : V(0);
+    return over_lanes<WAVES>(masked, [](V a, V b) { return a + b; });
+}
+
 // f over all threads of the workgroup.  part: LDS, one entry per wave; free again after the next barrier.
 template <int THREADS, typename V, typename F>
 __device__ __forceinline__ V block_all(V v, V *part, F f) {
     v = wave_all(v, f);
-    if (THREADS == 64) return v;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    V r = part[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) r = f(r, part[w]);
-    return r;
+    return across_waves<THREADS / 64>(part, f);
 }
 template <int THREADS, typename V>
 __device__ __forceinline__ V block_sum(V v, V *part) {

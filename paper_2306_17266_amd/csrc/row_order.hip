@@ -24,7 +24,7 @@ constexpr int MEMBERS = 256;            // that are ranked by comparing each wit
 constexpr int TOP_LIST = 2 * LOGITS_MAX_TOP;
 
 struct SearchLds {
-    u64 weight[BINS];
+    u64 weight[BINS + 1];  // (the last: of what is in no order)
     uint32_t count[BINS];
     u64 w[MEMBERS];  // members of the interval that is cut no further
     uint32_t key[MEMBERS];
@@ -68,8 +68,6 @@ struct Grid {
 #pragma clang fp contract(off)
         return (best - (double)z) * scale;
     }
-    // (an infinite maximum: everything in the last interval)
-    __device__ __forceinline__ int bin(double floor_of_place) const { return (int)fmin(floor_of_place, BINS - 1.0); }
     // Key of the smallest logit in intervals 0 .. b.
     __device__ uint32_t lowest_key(int b) const {
         const uint32_t lowest = KEY_NONE + 1, highest = order_key((float)best);
@@ -86,13 +84,19 @@ struct Grid {
 // (relative to it, 1 - 2^(-1/12) = 0.056 at most), in fixed point.
 struct Packed {
     int fraction, count_at;
-    __device__ __forceinline__ Packed(int n) : fraction(min(40, 66 - 2 * bits_of(n))), count_at(fraction - 4 + bits_of(n)) {}
+    double c[6];  // of the power series of 1 - 2^(-x / 12), what is left out 2e-11 at most, as fixed point
+    u64 one_more;
+    __device__ __forceinline__ Packed(int n) : fraction(min(40, 66 - 2 * bits_of(n))), count_at(fraction - 4 + bits_of(n)) {
+        constexpr double x = LN2 / BINS_PER_LOG2;
+        const double unit = ldexp(1.0, fraction);
+        c[0] = x * unit, c[1] = -x * x / 2 * unit, c[2] = x * x * x / 6 * unit, c[3] = -x * x * x * x / 24 * unit;
+        c[4] = x * x * x * x * x / 120 * unit, c[5] = -x * x * x * x * x * x / 720 * unit;
+        one_more = (1ull << count_at) - 0x4330000000000000ull;  // (less the bits of 2^52)
+    }
     __device__ __forceinline__ u64 one(double below) const {  // below: place - floor(place)
-        const double x = below * (LN2 / BINS_PER_LOG2);
-        double p = fma(x, 1.0 / 720, -1.0 / 120);
-        p = fma(p, x, 1.0 / 24), p = fma(p, x, -1.0 / 6), p = fma(p, x, 0.5), p = fma(p, x, -1.0);
-        const double v = 4503599627370496.0 - ldexp(p * x, fraction);
-        return (u64)__double_as_longlong(v) - 0x4330000000000000ull + (1ull << count_at);
+        double p = fma(c[5], below, c[4]);
+        p = fma(p, below, c[3]), p = fma(p, below, c[2]), p = fma(p, below, c[1]), p = fma(p, below, c[0]);
+        return (u64)__double_as_longlong(fma(p, below, 4503599627370496.0)) + one_more;
     }
     __device__ __forceinline__ uint32_t count(u64 v) const { return (uint32_t)(v >> count_at); }
     // Weight of interval b, relative to the largest logit's.
@@ -124,15 +128,9 @@ __device__ u64 find_bin(SearchLds &s, Limit &limit, float share, const uint32_t 
     if ((tid & 63) == 63) s.part32[wave] = n_upto, s.part64[wave] = w_upto;
     if (tid == 0) s.bin = -1;
     __syncthreads();
-#pragma unroll
-    for (int v = 0; v < THREADS / 64; ++v) {
-        const uint32_t pn = s.part32[v];
-        const u64 pw = s.part64[v];
-        n_before += v < wave ? pn : 0;
-        w_before += v < wave ? pw : 0;
-        total += pw;
-    }
-    n_before += n_upto - n_own, w_before += w_upto - w_own;
+    total = sum_across<THREADS / 64>(s.part64);
+    n_before += sum_before<THREADS / 64>(s.part32) + n_upto - n_own;
+    w_before += sum_before<THREADS / 64>(s.part64) + w_upto - w_own;
     if (share >= 0.0f) limit.weight = fmax((double)share * (double)total, 1.0);
     if (!limit.reached(n_before, w_before) && limit.reached(n_before + n_own, w_before + w_own)) {  // (one thread at most)
         bool found = false;
@@ -178,10 +176,7 @@ __device__ u64 sum_values(const HeldRow<T, N> &row, u64 (&own)[N], u64 *wave, fl
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = sum;
     __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += wave[w];
-    return sum;
+    return sum_across<THREADS / 64>(wave);
 }
 template <int THREADS, bool FEW, typename T, int N, typename F>
 __device__ u64 sum_values(const Row<T> &row, u64 (&)[N], u64 *wave, float z_low, F value) {
@@ -190,10 +185,7 @@ __device__ u64 sum_values(const Row<T> &row, u64 (&)[N], u64 *wave, float z_low,
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = sum;
     __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += wave[w];
-    return sum;
+    return sum_across<THREADS / 64>(wave);
 }
 
 // found(logit, index) in one thread, for the element of piece r (first index j) at which the running sum passes target, if it is
@@ -214,12 +206,10 @@ __device__ __forceinline__ void find_in_piece(uint4 r, int j, u64 own, u64 befor
 
 // found(logit, index), in one thread, for the first element in the order of the indexes at which the running sum of the values
 // exceeds target.  own, wave: as sum_values() left them.
-template <typename T, int N, typename F, typename G>
+template <int THREADS, typename T, int N, typename F, typename G>
 __device__ void first_beyond(const HeldRow<T, N> &row, const u64 (&own)[N], const u64 *wave, u64 target, F value, G found) {
-    const int me = threadIdx.x >> 6;
-    u64 before = 0;
-    for (int w = 0; w < me; ++w) before += wave[w];
-    if (before > target || before + wave[me] <= target) return;
+    u64 before = sum_before<THREADS / 64>(wave);
+    if (before > target || before + wave[threadIdx.x >> 6] <= target) return;
     uint4 r = row.raw[0];
     u64 sum = own[0];
     int at = 0;
@@ -233,12 +223,10 @@ __device__ void first_beyond(const HeldRow<T, N> &row, const u64 (&own)[N], cons
     }
     find_in_piece<T>(r, row.index(at), sum, before, target, value, found);
 }
-template <typename T, int N, typename F, typename G>
+template <int THREADS, typename T, int N, typename F, typename G>
 __device__ void first_beyond(const Row<T> &row, const u64 (&)[N], const u64 *wave, u64 target, F value, G found) {
-    const int me = threadIdx.x >> 6;
-    u64 before = 0;
-    for (int w = 0; w < me; ++w) before += wave[w];
-    if (before > target || before + wave[me] <= target) return;
+    u64 before = sum_before<THREADS / 64>(wave);
+    if (before > target || before + wave[threadIdx.x >> 6] <= target) return;
     for (int i = 0; i < row.rounds; ++i) {
         u64 own = 0;
         row.piece(i, [&](float z, int j) { own += value(z, j); });
@@ -273,7 +261,7 @@ __device__ __forceinline__ Cut cut_among(const R &row, const Weight &weight, Sea
             u64 own[N];
             __syncthreads();
             sum_values<THREADS, true>(row, own, s.part64, z_low, is_member);
-            first_beyond(row, own, s.part64, need - 1, is_member, [&](float, int j) { s.rank = j; });
+            first_beyond<THREADS>(row, own, s.part64, need - 1, is_member, [&](float, int j) { s.rank = j; });
             __syncthreads();
             return Cut{low, s.rank};
         }
@@ -338,7 +326,7 @@ struct Found {
 };
 
 // BY_WEIGHT: the limit has a weight, the share of the row's sum where share >= 0.  SUMS: the sums of Found (with what is
-// below the grid).
+// below the grid).  For rows with a finite maximum.
 template <int THREADS, bool BY_WEIGHT, bool SUMS, typename R>
 __device__ Found search_grid(const R &row, const Weight &weight, const Grid &grid, SearchLds &s, double *part_d, Limit &limit, float share, int n,
                              int fraction) {
@@ -347,18 +335,10 @@ __device__ Found search_grid(const R &row, const Weight &weight, const Grid &gri
     for (int b = threadIdx.x; b < BINS; b += THREADS) s.weight[b] = 0;
     if (threadIdx.x == 0) s.before = 0, s.weight_before = 0;
     __syncthreads();
-    double tail = 0.0;
     row.each([&](float z, int) {
-        if (z > -INFINITY) {
-            const double t = grid.place(z), g = floor(t);
-            const int b = grid.bin(g);
-            if (SUMS && b == BINS - 1) {
-                atomicAdd(&s.weight[b], 1ull << packed.count_at);
-                tail += exp2_64<7>(weight.log2_of(z));
-            } else {
-                atomicAdd(&s.weight[b], packed.one(t - g));
-            }
-        }
+        const double t = grid.place(z), g = floor(t);
+        const int b = min((int)g, BINS - 1);
+        atomicAdd(&s.weight[z > -INFINITY ? b : BINS], packed.one(t - g));  // (no branch: it would be one for each logit)
     });
     __syncthreads();
     uint32_t count[OWN];
@@ -377,8 +357,15 @@ __device__ Found search_grid(const R &row, const Weight &weight, const Grid &gri
     find_bin<THREADS>(s, limit, share, count, w);
     Found f{1, 0, 0.0, 0.0};
     const int bin = s.bin;
-    if (bin >= 0) f.low = grid.lowest_key(bin), f.high = bin > 0 && !weight.infinite ? grid.lowest_key(bin - 1) - 1 : 0xFFFFFFFFu;
+    if (bin >= 0) f.low = grid.lowest_key(bin), f.high = bin > 0 ? grid.lowest_key(bin - 1) - 1 : 0xFFFFFFFFu;
     if (SUMS) {
+        double tail = 0.0;
+        if (packed.count(s.weight[BINS - 1])) {
+            const uint32_t last = grid.lowest_key(BINS - 2);
+            row.each([&](float z, int) {
+                if (order_key(z) < last) tail += exp2_64<6>(weight.log2_of(z));
+            });
+        }
         double below = 0.0, total = tail;
 #pragma unroll
         for (int i = 0; i < OWN; ++i) total += wd[i], below += bin >= 0 && threadIdx.x * OWN + i > bin ? wd[i] : 0.0;
@@ -404,13 +391,13 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a, int ro
     __shared__ SearchLds s;
     const long r = (long)row0 + blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Source<T, N> row(a.in, r, wave, THREADS / 64, lane);
+    Source<T, N> row(a.in, r, wave, THREADS / 64, lane);
     const float temperature = a.temperature ? a.temperature[r] : 1.0f;
     const int k = a.top_k && a.top_k[r] > 0 ? min(a.top_k[r], a.in.n) : a.in.n;
     const float top_p = a.top_p ? a.top_p[r] : 1.0f;
     const float min_p = a.min_p ? fminf(fmaxf(a.min_p[r], 0.0f), 1.0f) : 0.0f;
     const float uniform = a.uniform[r];
-    const float best = largest<THREADS>(row, s.part_f);
+    float best = largest<THREADS>(row, s.part_f);
     if (best == -INFINITY) {  // nothing to draw from
         if (threadIdx.x == 0) {
             a.classes[r] = -1;
@@ -429,6 +416,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a, int ro
         return;
     }
     const double inv_t = 1.0 / (double)temperature;
+    if (best == INFINITY) row.only_infinite(), best = 0.0f;
     const Weight weight(best, inv_t);
     const int fraction = fraction_bits(a.in.n);
     const double t_min = min_p > 0.0f ? log2((double)min_p) : -INFINITY;
@@ -436,19 +424,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a, int ro
     Cut cut = keep_all();
     if (by_weight || k < a.in.n) {
         Limit limit{(uint32_t)k, INFINITY};
-        Found f{0xFF800000u, 0xFF800000u, 0.0, 0.0};
-        if (weight.infinite) {  // equal shares for the infinite ones
-            uint32_t n = 0;
-            row.each([&](float z, int) { n += z == INFINITY; });
-            n = block_sum<THREADS>(n, s.part32);
-            if (threadIdx.x == 0) s.before = 0, s.weight_before = 0, s.inside = n;
-            __syncthreads();
-            if (by_weight) limit.weight = fmax((double)fmaxf(top_p, 0.0f) * (double)((u64)n << fraction), 1.0);
-            if (!limit.reached(n, (u64)n << fraction)) f.low = 1, f.high = 0;
-        } else {
-            const Grid grid(best, inv_t);
-            f = search_grid<THREADS, true, false>(row, weight, grid, s, nullptr, limit, by_weight ? fmaxf(top_p, 0.0f) : -1.0f, a.in.n, fraction);
-        }
+        const Found f = search_grid<THREADS, true, false>(row, weight, Grid(best, inv_t), s, nullptr, limit, by_weight ? fmaxf(top_p, 0.0f) : -1.0f, a.in.n, fraction);
         if (f.low <= f.high) cut = cut_among<THREADS, true, N ? N : 1>(row, weight, s, limit, f.low, f.high, fraction);
     }
     auto kept = [&](float z, int j) {
@@ -465,7 +441,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleArgs a, int ro
                           : sum_values<THREADS, false>(row, own, s.part64, -INFINITY, [&](float z, int) { return fixed_weight(weight.log2_of(z), fraction); });
     const double u = fminf(fmaxf(uniform, 0.0f), 1.0f - 5.9604645e-08f);  // (into [0, 1); NaN: 0)
     const u64 target = min((u64)(u * (double)total), total - 1);
-    first_beyond(row, own, s.part64, target, kept, [&](float z, int j) {
+    first_beyond<THREADS>(row, own, s.part64, target, kept, [&](float z, int j) {
         a.classes[r] = j;
         if (a.log_prob) a.log_prob[r] = (float)((weight.log2_of(z) + fraction - log2((double)total)) * LN2);
     });
@@ -482,10 +458,20 @@ __global__ __launch_bounds__(THREADS, 4) void top_logits_kernel(TopArgs a, int r
     const Source<T, N> row(a.in, r, wave, THREADS / 64, lane);
     const float best = largest<THREADS>(row, s.part_f);
     const double inv_t = 1.0 / (double)a.temperature;
-    const Weight weight(best, inv_t);
+    const bool infinite = best == INFINITY;
+    const Weight weight(infinite ? 0.0f : best, inv_t);
     Limit limit{(uint32_t)a.k, INFINITY};
     Found f{1, 0, 0.0, 1.0};
-    if (best > -INFINITY) f = search_grid<THREADS, false, true>(row, weight, Grid(best, inv_t), s, part[0], limit, -1.0f, a.in.n, 0);
+    if (infinite) {  // (the grid ends there: cut by keys alone)
+        uint32_t ordered = 0, infinities = 0;
+        row.each([&](float z, int) { ordered += z > -INFINITY, infinities += z == INFINITY; });
+        ordered = block_sum<THREADS>(ordered, s.part32);
+        infinities = block_sum<THREADS>(infinities, reinterpret_cast<uint32_t *>(s.part64));
+        if (threadIdx.x == 0) s.before = 0, s.weight_before = 0, s.inside = ordered;
+        __syncthreads();
+        f.total = infinities;
+        if ((int)ordered >= a.k) f.low = KEY_NONE + 1, f.high = 0xFFFFFFFFu;
+    } else if (best > -INFINITY) f = search_grid<THREADS, false, true>(row, weight, Grid(best, inv_t), s, part[0], limit, -1.0f, a.in.n, 0);
     // everything down to the interval of the k-th, or, if that holds too much, down to the k-th itself
     Cut cut = keep_all();
     const bool all = f.low <= f.high && s.before + s.inside <= TOP_LIST;
@@ -501,7 +487,7 @@ __global__ __launch_bounds__(THREADS, 4) void top_logits_kernel(TopArgs a, int r
         if (cut.keeps(k, j))
             order[min(atomicAdd(&n_listed, 1), TOP_LIST - 1)] = (u64)k << 32 | (uint32_t)~j;
         else if (k <= f.high)
-            outside += exp2_64<7>(weight.log2_of(z));
+            outside += exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
     });
     __syncthreads();
     // sorted in LDS: keys above inverted indexes
@@ -525,7 +511,8 @@ __global__ __launch_bounds__(THREADS, 4) void top_logits_kernel(TopArgs a, int r
             a.values[r * a.k + i] = v ? key_value((uint32_t)(v >> 32)) : -INFINITY;
             a.classes[r * a.k + i] = v ? (int)~(uint32_t)v : -1;
         } else {
-            outside += exp2_64<7>(weight.log2_of(key_value((uint32_t)(v >> 32))));
+            const float z = key_value((uint32_t)(v >> 32));
+            outside += exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
         }
     }
     outside = block_sum<THREADS>(outside, part[2]);
