@@ -368,21 +368,19 @@ hipError_t launch_held(const DistillArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
-// (for both types alike: the workspace's size does not depend on it, and float32 has more parts)
-int rows_of_slice(int rows, int n) { return (int)std::min<long>(LOGITS_SLICE / logits_parts(n, false), rows); }
-
 template <typename T>
 hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
-    constexpr int PER = 16 / sizeof(T);
-    const int pieces = (a.in.n + 2 * PER - 2) / PER;  // (a row may start inside its first piece)
+    const int pieces = logits_pieces(a.in.n, a.in.bf16);
     const bool together = !a.grad || ((reinterpret_cast<uintptr_t>(a.grad) - reinterpret_cast<uintptr_t>(a.in.x)) % 16 == 0 &&
                                       (a.in.rows == 1 || (a.grad_stride - a.in.stride) * (long)sizeof(T) % 16 == 0));
-    if (together && pieces <= 256) return launch_held<T, 1, 256>(a, s);
-    if (together && pieces <= 1024) return launch_held<T, 4, 256>(a, s);
-    if (together && pieces <= 4096) return launch_held<T, 8, 512>(a, s);
-    if (together && pieces <= 8192 && a.in.rows >= 256) return launch_held<T, 8, 1024>(a, s);
+    if (together && held_rows(a.in)) {
+        if (pieces <= 256) return launch_held<T, 1, 256>(a, s);
+        if (pieces <= 1024) return launch_held<T, 4, 256>(a, s);
+        if (pieces <= 4096) return launch_held<T, 8, 512>(a, s);
+        return launch_held<T, 8, 1024>(a, s);
+    }
     const int parts = logits_parts(a.in.n, a.in.bf16);
-    const int most = rows_of_slice(a.in.rows, a.in.n);
+    const long most = std::min<long>(rows_of_slice(a.in.n), a.in.rows);
     RowSums *rows = reinterpret_cast<RowSums *>(ws);
     PartSums *sums = reinterpret_cast<PartSums *>(ws + most * sizeof(RowSums));
     for (long first = 0; first < a.in.rows; first += most) {
@@ -398,8 +396,13 @@ hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
 
 }  // namespace
 
+size_t distill_part_bytes() { return sizeof(PartSums); }
+size_t distill_row_bytes() { return sizeof(RowSums); }
+
 size_t logits_workspace_bytes(int rows, int n) {
-    return rows_of_slice(rows, n) * (sizeof(RowSums) + logits_parts(n, false) * sizeof(PartSums));
+    const size_t slice = std::min<long>(rows_of_slice(n), rows), parts = slice * logits_parts(n, false);
+    return std::max({parts * distill_part_bytes() + slice * distill_row_bytes(), parts * sample_part_bytes() + slice * sample_row_bytes(),
+                     parts * top_logits_part_bytes()});
 }
 
 hipError_t launch_distill(const DistillArgs &a, void *ws, hipStream_t s) {

@@ -54,14 +54,29 @@ struct DistillArgs {
     long grad_stride;  // elements from row to row
 };
 
-// Pieces of 16 bytes that a workgroup of the kernels for parts of rows takes, and parts that go out in one launch (what a
-// call needs of the workspace stays bounded).
+// Rows are read in pieces of 16 bytes.  A row that fits the registers of a workgroup is one workgroup's; longer rows, and long ones
+// where there are few, are read in parts of LOGITS_PART_PIECES, a workgroup each, whose results a workgroup per row joins.
 constexpr int LOGITS_PART_PIECES = 2048;
-constexpr long LOGITS_SLICE = 1 << 20;
-inline int logits_parts(int n, bool bf16) {  // (a row may start inside its first piece)
+inline int logits_pieces(int n, bool bf16) {  // (a row may start inside its first piece)
     const int per = bf16 ? 8 : 4;
-    return ((n + 2 * per - 2) / per + LOGITS_PART_PIECES - 1) / LOGITS_PART_PIECES;
+    return (n + 2 * per - 2) / per;
 }
+inline int logits_parts(int n, bool bf16) { return (logits_pieces(n, bf16) + LOGITS_PART_PIECES - 1) / LOGITS_PART_PIECES; }
+inline bool held_rows(const LogitRows &in) {
+    const int pieces = logits_pieces(in.n, in.bf16);
+    return pieces <= 1024 || (pieces <= 8192 && in.rows >= 192);
+}
+// Rows that go out in one launch in parts (for both types alike): what a call needs of the workspace stays bounded.
+inline long rows_of_slice(int n) {
+    const long rows = 4096 / logits_parts(n, false);
+    return rows > 1 ? rows : 1;
+}
+// Of the workspace: bytes that an operator needs for each part, and for each row.
+size_t top_logits_part_bytes();
+size_t sample_part_bytes();
+size_t sample_row_bytes();
+size_t distill_part_bytes();
+size_t distill_row_bytes();
 
 // Bytes of scratch memory that every operator gets by with on rows of n logits.
 size_t logits_workspace_bytes(int rows, int n);

@@ -1,0 +1,549 @@
+// One class per row from given random numbers, under temperature, top-k, top-p and min-p (logits.h).
+//
+// The position at which top-k and top-p cut the order is searched with a histogram over a grid on the logits, 12 intervals for each
+// factor 2 of the weight, and then among the members of one interval (row_order.h).  The answer is found in the order of the
+// indexes: sums of the kept weights by waves and pieces, then the piece in which the running sum passes u times the whole.
+#include "row_order.h"
+
+namespace sushi {
+
+namespace {
+
+constexpr double BINS_PER_LOG2 = 12.0;  // 1024: down to 2^-85 of the largest weight, the rest in the last one
+
+// The grid: a logit lies in interval floor(place), counted downwards from the largest logit's.
+struct Grid {
+    double anchor, scale, top;  // place 0; intervals per unit of the logits; the largest logit's interval
+    // (rounded by itself: fused with a subtraction it would be another number in each use)
+    __device__ __forceinline__ double place(float z) const {
+#pragma clang fp contract(off)
+        return (anchor - (double)z) * scale;
+    }
+    __device__ __forceinline__ Grid(float best, double inv_t, double anchor_) : anchor(anchor_), scale(inv_t * (1.4426950408889634074 * BINS_PER_LOG2)) { top = floor(place(best)); }
+    // Key of the smallest logit in intervals 0 .. b.
+    __device__ uint32_t lowest_key(int b, float best) const {
+        const uint32_t lowest = KEY_NONE + 1, highest = order_key(best);
+        const double x = top + (b + 1.0);
+        if (b >= BINS - 1 || !(scale > 0.0)) return lowest;
+        uint32_t k = order_key((float)fmin(fmax(anchor - x / scale, -3.4028234663852886e38), 3.4028234663852886e38));
+        while (k > lowest && place(key_value(k - 1)) < x) --k;
+        while (k < highest && place(key_value(k)) >= x) ++k;
+        return k;
+    }
+};
+
+// An interval of the grid's histogram in one word: how many, above the sum of what their weights lack of the interval's upper end
+// (relative to it, 1 - 2^(-1/12) = 0.056 at most), in fixed point.
+struct Packed {
+    int fraction, count_at;
+    double c[6];  // of the power series of 1 - 2^(-x / 12), what is left out 2e-11 at most, as fixed point
+    u64 one_more;
+    __device__ __forceinline__ Packed(int n) : fraction(min(40, 66 - 2 * bits_of(n))), count_at(fraction - 4 + bits_of(n)) {
+        constexpr double x = LN2 / BINS_PER_LOG2;
+        const double unit = ldexp(1.0, fraction);
+        c[0] = x * unit, c[1] = -x * x / 2 * unit, c[2] = x * x * x / 6 * unit, c[3] = -x * x * x * x / 24 * unit;
+        c[4] = x * x * x * x * x / 120 * unit, c[5] = -x * x * x * x * x * x / 720 * unit;
+        one_more = (1ull << count_at) - 0x4330000000000000ull;  // (less the bits of 2^52)
+    }
+    __device__ __forceinline__ u64 one(double below) const {  // below: place - floor(place)
+        double p = fma(c[5], below, c[4]);
+        p = fma(p, below, c[3]), p = fma(p, below, c[2]), p = fma(p, below, c[1]), p = fma(p, below, c[0]);
+        return (u64)__double_as_longlong(fma(p, below, 4503599627370496.0)) + one_more;
+    }
+    __device__ __forceinline__ uint32_t count(u64 v) const { return (uint32_t)(v >> count_at); }
+    __device__ __forceinline__ u64 lack(u64 v) const { return v & ((1ull << count_at) - 1); }
+    // Weight of count members of which so much is lacking of the weight 2^t each.
+    __device__ __forceinline__ double weight(uint32_t count, u64 lacking, double t) const { return ((double)count - ldexp((double)lacking, -fraction)) * exp2_64<11>(t); }
+};
+
+// The histogram of what a source holds, in s.weight.
+template <int THREADS, typename R>
+__device__ void build_histogram(const R &row, const Grid &grid, const Packed &packed, SearchLds &s) {
+    for (int b = threadIdx.x; b < BINS; b += THREADS) s.weight[b] = 0;
+    __syncthreads();
+    row.each([&](float z, int) {
+        const double t = grid.place(z), g = floor(t);
+        const int b = min((int)(g - grid.top), BINS - 1);
+        atomicAdd(&s.weight[z > -INFINITY ? b : BINS], packed.one(t - g));  // (no branch: it would be one for each logit)
+    });
+    __syncthreads();
+}
+
+// The keys of the interval in which the limit is reached; low > high: in none.  share >= 0: that share of the row's sum is the limit's
+// weight.  count, lacking: this thread's run of intervals.  equal: members of the first that equal the maximum and are in neither.
+struct Range {
+    uint32_t low, high;
+};
+template <int THREADS>
+__device__ Range search(SearchLds &s, const Grid &grid, const Packed &packed, float best, Limit &limit, float share, uint32_t (&count)[BINS / THREADS],
+                        const u64 (&lacking)[BINS / THREADS], uint32_t equal, int fraction) {
+    constexpr int OWN = BINS / THREADS;
+    const double above = grid.place(best) - grid.top;  // of the maximum within its interval
+    u64 w[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int b = threadIdx.x * OWN + i;
+        double wd = count[i] && b < BINS - 1 ? packed.weight(count[i], lacking[i], (above - b) * (1.0 / BINS_PER_LOG2)) : 0.0;
+        if (b == 0) count[i] += equal, wd += equal;
+        w[i] = (u64)ldexp(wd, fraction);
+    }
+    find_bin<THREADS>(s, limit, share, count, w);
+    const int bin = s.bin;
+    if (bin < 0) return Range{1, 0};
+    return Range{grid.lowest_key(bin, best), bin > 0 ? grid.lowest_key(bin - 1, best) - 1 : 0xFFFFFFFFu};
+}
+
+// How a row is drawn from.
+struct Draw {
+    float temperature, top_p, min_p, u;
+    int k;
+    bool first;  // the first of the order, whatever else is asked for
+    __device__ __forceinline__ Draw(const SampleArgs &a, long r) {
+        temperature = a.temperature ? a.temperature[r] : 1.0f;
+        k = a.top_k && a.top_k[r] > 0 ? min(a.top_k[r], a.in.n) : a.in.n;
+        top_p = a.top_p ? a.top_p[r] : 1.0f;
+        min_p = a.min_p ? fminf(fmaxf(a.min_p[r], 0.0f), 1.0f) : 0.0f;
+        u = fminf(fmaxf(a.uniform[r], 0.0f), 1.0f - 5.9604645e-08f);  // (into [0, 1); NaN: 0)
+        first = !(temperature > 0.0f);
+        if (first) temperature = 1.0f, k = 1, top_p = 1.0f, min_p = 0.0f;
+    }
+    __device__ __forceinline__ bool cuts(int n) const { return k < n || top_p < 1.0f; }
+    __device__ __forceinline__ float share() const { return top_p < 1.0f ? fmaxf(top_p, 0.0f) : -1.0f; }
+    __device__ __forceinline__ double t_min() const { return min_p > 0.0f ? log2((double)min_p) : -INFINITY; }
+};
+
+// Which logits are kept, and their weights.
+struct Kept {
+    Weight weight;
+    Cut cut;
+    double t_min;
+    int fraction;
+    __device__ __forceinline__ u64 operator()(float z, int j) const {
+        const double t = weight.log2_of(z);
+        return cut.keeps(order_key(z), j) && t >= t_min ? fixed_weight(t, fraction) : 0;
+    }
+    // What is below has no weight (min_p's border a little lowered: the exact test is above).
+    __device__ __forceinline__ float lowest() const {
+        double z = weight.best + t_min / weight.scale;
+        z -= fabs(z) * 1e-6;
+        return fmaxf(key_value(cut.key), z > -3e38 && z < 3e38 ? (float)z : -INFINITY);
+    }
+};
+
+__device__ __forceinline__ u64 target_of(float u, u64 total) { return min((u64)((double)u * (double)total), total - 1); }
+
+__device__ __forceinline__ void write_answer(const SampleArgs &a, long r, int j, double log2_of, int fraction, u64 total) {
+    a.classes[r] = j;
+    if (a.log_prob) a.log_prob[r] = (float)((log2_of + fraction - log2((double)total)) * LN2);
+}
+__device__ __forceinline__ void write_nothing(const SampleArgs &a, long r) {  // (nothing to draw from)
+    a.classes[r] = -1;
+    if (a.log_prob) a.log_prob[r] = -INFINITY;
+}
+
+// Sums of value(logit, index) by pieces and over what the workgroup holds; wave[w]: LDS, the part of wave w.  Only what is at least
+// z_low has a value; FEW: which is not much.
+template <int THREADS, bool FEW, typename T, int N, typename F>
+__device__ u64 sum_values(const HeldRow<T, N> &row, u64 (&own)[N], u64 *wave, float z_low, F value) {
+    u64 sum = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        own[i] = 0;
+        if (i < row.rounds) {
+            const int j = row.index(i);
+            if (FEW) {
+                from_piece<T>(row.raw[i], j, z_low, [&](float z, int at) { own[i] += value(z, at); });
+            } else {
+                float v[HeldRow<T, N>::PER];
+                unpack<T>(row.raw[i], v);
+#pragma unroll
+                for (int e = 0; e < HeldRow<T, N>::PER; ++e) own[i] += value(v[e], j + e);
+            }
+            apart();
+        }
+        sum += own[i];
+    }
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    return sum_across<THREADS / 64>(wave);
+}
+
+// found(logit, index), in one thread, for the first element in the order of the indexes at which the running sum of the values
+// exceeds target.  own, wave: as sum_values() left them.
+template <int THREADS, typename T, int N, typename F, typename G>
+__device__ void first_beyond(const HeldRow<T, N> &row, const u64 (&own)[N], const u64 *wave, u64 target, F value, G found) {
+    u64 before = sum_before<THREADS / 64>(wave);
+    if (before > target || before + wave[threadIdx.x >> 6] <= target) return;
+    uint4 r = row.raw[0];
+    u64 sum = own[0];
+    int at = 0;
+    bool passed = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const u64 all = wave_sum(own[i]);
+        r = choose(passed, r, row.raw[i]), sum = passed ? sum : own[i], at = passed ? at : i;
+        passed |= before + all > target;
+        before += passed ? 0 : all;
+    }
+    find_in_piece<T>(r, row.index(at), sum, before, target, value, found);
+}
+
+// ------------------------------------------------------------------ a row in the registers of a workgroup
+
+template <typename T, int N, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, int row0) {
+    __shared__ SearchLds s;
+    const long r = (long)row0 + blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    HeldRow<T, N> row(a.in, r, wave, THREADS / 64, lane);
+    const Draw draw(a, r);
+    float best = largest<THREADS>(row, s.part_f);
+    if (best == -INFINITY) {
+        if (threadIdx.x == 0) write_nothing(a, r);
+        return;
+    }
+    const double inv_t = 1.0 / (double)draw.temperature;
+    const bool infinite = best == INFINITY;
+    if (infinite) row.only_infinite(), best = 0.0f;
+    Kept kept{Weight(best, inv_t), keep_all(), draw.t_min(), fraction_bits(a.in.n)};
+    if (draw.cuts(a.in.n)) {
+        constexpr int OWN = BINS / THREADS;
+        const Grid grid(best, inv_t, best);  // (the largest logit is place 0: a row of equal logits has exact sums, and its cut is where the count says)
+        const Packed packed(a.in.n);
+        if (threadIdx.x == 0) s.before = 0, s.weight_before = 0;
+        build_histogram<THREADS>(row, grid, packed, s);
+        uint32_t count[OWN];
+        u64 lacking[OWN];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const u64 v = s.weight[threadIdx.x * OWN + i];
+            count[i] = packed.count(v), lacking[i] = packed.lack(v);
+        }
+        Limit limit{(uint32_t)draw.k, INFINITY};
+        const Range f = search<THREADS>(s, grid, packed, best, limit, draw.share(), count, lacking, 0, kept.fraction);
+        if (f.low <= f.high) {
+            Row<T> whole(a.in, r, wave, THREADS / 64, lane);
+            if (infinite) whole.only_infinite();
+            kept.cut = cut_among<THREADS, true>(row, whole, kept.weight, s, limit, f.low, f.high, kept.fraction);
+            __syncthreads();
+        }
+    }
+    u64 own[N];
+    const u64 total = draw.cuts(a.in.n) || draw.min_p > 0.0f
+                          ? sum_values<THREADS, true>(row, own, s.part64, kept.lowest(), kept)
+                          : sum_values<THREADS, false>(row, own, s.part64, -INFINITY, [&](float z, int) { return fixed_weight(kept.weight.log2_of(z), kept.fraction); });
+    first_beyond<THREADS>(row, own, s.part64, target_of(draw.u, total), kept, [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
+}
+
+// ------------------------------------------------------------------ a row in parts
+
+constexpr int PART_THREADS = 256, PART_ROUNDS = LOGITS_PART_PIECES / PART_THREADS, JOIN_THREADS = 1024;
+constexpr int JOIN_ROUNDS = LOGITS_PART_PIECES / JOIN_THREADS;
+constexpr int LIST = 4096;  // members of the interval in which a row is cut that are kept for its last step
+constexpr int MOST_PARTS = LOGITS_MAX_CLASSES / (4 * LOGITS_PART_PIECES) + 1;
+
+// What a part has of its row: its maximum and how often; the histogram over a grid that all parts of the row share (place 0 is the
+// logit 0), from the maximum's interval on, without what equals the maximum; or, without filters, the sum of its weights.
+struct SamplePart {
+    float best;
+    uint32_t equal, ordered;  // logits that equal the maximum, that are above -inf
+    double top, sum;
+    u64 kept;  // sum of the weights that are kept whatever the list says
+    u64 weight[BINS];
+};
+// What the parts need to know of their row once the histograms are joined.
+struct SampleRow {
+    float best;
+    uint32_t low, high;  // the interval in which the row is cut (low > high: none)
+    uint32_t before, inside;
+    u64 weight_before;
+    double limit;
+    int n;  // listed
+    u64 entry[LIST];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ HeldRow<T, N> part_row(const SampleArgs &a, long r, int part, int threads) {
+    return HeldRow<T, N>(a.in, r, threadIdx.x >> 6, threads / 64, threadIdx.x & 63, part * LOGITS_PART_PIECES, LOGITS_PART_PIECES);
+}
+
+// First launch.  CUT: histograms; else sums.
+template <typename T, bool CUT>
+__global__ __launch_bounds__(PART_THREADS) void sample_part_kernel(SampleArgs a, int row0, int parts, SamplePart *out) {
+    __shared__ SearchLds s;
+    __shared__ double part_d[PART_THREADS / 64];
+    const long r = (long)row0 + blockIdx.x / parts;
+    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
+    const Draw draw(a, r);
+    SamplePart &mine = out[blockIdx.x];
+    const float m = largest<PART_THREADS>(row, s.part_f);
+    const float best = m == INFINITY ? 0.0f : m;
+    if (threadIdx.x == 0) mine.best = m;
+    if (m == -INFINITY) return;
+    if (m == INFINITY) row.only_infinite();
+    const double inv_t = 1.0 / (double)draw.temperature;
+    if (!CUT) {
+        const Weight weight(best, inv_t);
+        double sum = 0.0;
+        row.each([&](float z, int) { sum += exp2_64<11>(weight.log2_of(z)); });
+        sum = block_sum<PART_THREADS>(sum, part_d);
+        if (threadIdx.x == 0) mine.sum = sum;
+        return;
+    }
+    const Grid grid(best, inv_t, 0.0);
+    const Packed packed(LOGITS_PART_PIECES * HeldRow<T, PART_ROUNDS>::PER);
+    build_histogram<PART_THREADS>(row, grid, packed, s);
+    u64 both = 0;
+    row.each([&](float z, int) { both += (u64)(z == best) + ((u64)(z > -INFINITY) << 32); });
+    both = block_sum<PART_THREADS>(both, s.part64);
+    if (threadIdx.x == 0) {
+        const double t = grid.place(best);
+        s.weight[0] -= (both & 0xFFFFFFFFu) * packed.one(t - floor(t));
+        mine.equal = (uint32_t)both, mine.ordered = (uint32_t)(both >> 32), mine.top = grid.top;
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < BINS; b += PART_THREADS) mine.weight[b] = s.weight[b];
+}
+
+// Second launch, a workgroup per row: the joined histogram, and where the row is cut.
+__global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a, int row0, int parts, const SamplePart *in, SampleRow *out) {
+    __shared__ SearchLds s;
+    __shared__ double top[MOST_PARTS];
+    __shared__ float maxima[MOST_PARTS];
+    static_assert(BINS == JOIN_THREADS, "a thread has one interval");
+    const long r = (long)row0 + blockIdx.x;
+    in += (long)blockIdx.x * parts;
+    SampleRow &row = out[blockIdx.x];
+    const Draw draw(a, r);
+    float m = -INFINITY;
+    if ((int)threadIdx.x < parts) m = maxima[threadIdx.x] = in[threadIdx.x].best, top[threadIdx.x] = in[threadIdx.x].top;
+    m = block_all<JOIN_THREADS>(m, s.part_f, [](float p, float q) { return fmaxf(p, q); });
+    if (threadIdx.x == 0) row.best = m, row.n = 0, row.low = 1, row.high = 0, s.before = 0, s.weight_before = 0;
+    if (m == -INFINITY || !draw.cuts(a.in.n)) return;
+    const float best = m == INFINITY ? 0.0f : m;
+    const int fraction = fraction_bits(a.in.n);
+    const Grid grid(best, 1.0 / (double)draw.temperature, 0.0);
+    const Packed packed(LOGITS_PART_PIECES * (a.in.bf16 ? 8 : 4));
+    __syncthreads();
+    uint32_t count[1] = {0}, equal = 0, ordered = 0;
+    u64 lacking[1] = {0};
+    for (int p = 0; p < parts; ++p) {
+        if (maxima[p] == -INFINITY || (m == INFINITY && maxima[p] < INFINITY)) continue;
+        // the part's intervals lie `down` further down
+        const int down = (int)fmin(top[p] - grid.top, (double)BINS), b = (int)threadIdx.x - down;
+        ordered += in[p].ordered;
+        if (maxima[p] == m) equal += in[p].equal;
+        if (b >= 0 && threadIdx.x < BINS - 1) {
+            const u64 v = in[p].weight[b];
+            count[0] += packed.count(v), lacking[0] += packed.lack(v);
+            if (b == 0 && maxima[p] < m) {  // what equals the part's maximum, at its own place
+                const double t = grid.place(maxima[p]);
+                count[0] += in[p].equal, lacking[0] += in[p].equal * packed.lack(packed.one(t - floor(t)));
+            }
+        }
+    }
+    // what falls off the end, in the last interval
+    const uint32_t placed = block_sum<JOIN_THREADS>(count[0], s.part32);
+    if (threadIdx.x == BINS - 1) count[0] = ordered - placed - equal;
+    __syncthreads();
+    Limit limit{(uint32_t)draw.k, INFINITY};
+    const Range f = search<JOIN_THREADS>(s, grid, packed, best, limit, draw.share(), count, lacking, equal, fraction);
+    if (threadIdx.x == 0)
+        row.low = f.low, row.high = f.high, row.before = s.before, row.inside = s.inside, row.weight_before = s.weight_before, row.limit = limit.weight;
+}
+
+// Third launch: each part lists its members of that interval, and sums what is kept above it.
+template <typename T>
+__global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs a, int row0, int parts, SamplePart *part_out, SampleRow *rows) {
+    __shared__ u64 part64[PART_THREADS / 64];
+    __shared__ int n, at;
+    const long r = (long)row0 + blockIdx.x / parts;
+    SampleRow &state = rows[blockIdx.x / parts];
+    SamplePart &mine = part_out[blockIdx.x];
+    const float m = state.best;
+    const uint32_t low = state.low, high = state.high;
+    const Draw draw(a, r);
+    const bool cut = low <= high;
+    Kept kept{Weight(m == INFINITY ? 0.0f : m, 1.0 / (double)draw.temperature), cut ? Cut{high, -1} : keep_all(), draw.t_min(), fraction_bits(a.in.n)};
+    const float z_low = cut ? key_value(low) : kept.lowest();
+    const float own = m == INFINITY ? (mine.best == INFINITY ? 0.0f : -INFINITY) : mine.best;
+    if (m == -INFINITY || !(own >= z_low)) {  // (nothing here)
+        if (threadIdx.x == 0) mine.kept = 0;
+        return;
+    }
+    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
+    if (m == INFINITY) row.only_infinite();
+    if (threadIdx.x == 0) n = 0;
+    __syncthreads();
+    u64 sum = 0;
+    int members = 0;
+    row.each_from(z_low, [&](float z, int j) {
+        const uint32_t k = order_key(z);
+        sum += kept(z, j);
+        members += cut && k >= low && k <= high;
+    });
+    // a run of the row's list for this part's members
+    int before = wave_scan(members);
+    const int all = __shfl(before, 63), lane = threadIdx.x & 63;
+    int wave_at = 0;
+    if (lane == 0 && all) wave_at = atomicAdd(&n, all);
+    before += __shfl(wave_at, 0) - members;
+    sum = wave_sum(sum);
+    if (lane == 0) part64[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (n) at = atomicAdd(&state.n, n);
+        mine.kept = part64[0] + part64[1] + part64[2] + part64[3];
+    }
+    __syncthreads();
+    before += at;
+    if (members)
+        row.each_from(z_low, [&](float z, int j) {
+            const uint32_t k = order_key(z);
+            if (cut && k >= low && k <= high) {
+                if (before < LIST) state.entry[before] = (u64)k << 32 | (uint32_t)j;
+                ++before;
+            }
+        });
+}
+
+// A row's list.
+struct Listed {
+    const u64 *entry;
+    int n;
+    template <typename F>
+    __device__ __forceinline__ void each_from(float z_low, F f) const {
+        const uint32_t low = order_key(z_low);
+        for (int i = threadIdx.x; i < n; i += JOIN_THREADS)
+            if ((uint32_t)(entry[i] >> 32) >= low) f(key_value((uint32_t)(entry[i] >> 32)), (int)(uint32_t)entry[i]);
+    }
+};
+
+// Last launch, a workgroup per row: the cut, the part in which the running sum passes the target, and the class there.
+template <typename T, bool CUT>
+__global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs a, int row0, int parts, const SamplePart *in, const SampleRow *rows) {
+    __shared__ SearchLds s;
+    __shared__ u64 sums[MOST_PARTS];
+    __shared__ int chosen;
+    __shared__ u64 chosen_before;
+    constexpr int PER = 16 / sizeof(T);
+    const long r = (long)row0 + blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    in += (long)blockIdx.x * parts;
+    const Draw draw(a, r);
+    Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
+    float m = -INFINITY;
+    if ((int)threadIdx.x < parts) m = in[threadIdx.x].best;
+    const float mine = m;
+    m = block_all<JOIN_THREADS>(m, s.part_f, [](float p, float q) { return fmaxf(p, q); });
+    if (m == -INFINITY) {
+        if (threadIdx.x == 0) write_nothing(a, r);
+        return;
+    }
+    if (m == INFINITY) whole.only_infinite();
+    const float best = m == INFINITY ? 0.0f : m;
+    Kept kept{Weight(best, 1.0 / (double)draw.temperature), keep_all(), draw.t_min(), fraction_bits(a.in.n)};
+    if (CUT) {
+        const SampleRow &state = rows[blockIdx.x];
+        const uint32_t low = state.low, high = state.high;
+        if (threadIdx.x == 0) s.before = state.before, s.weight_before = state.weight_before, s.inside = state.inside;
+        if ((int)threadIdx.x < parts) sums[threadIdx.x] = in[threadIdx.x].kept;
+        __syncthreads();
+        if (low <= high) {
+            const Limit limit{(uint32_t)draw.k, state.limit};
+            const Listed listed{state.entry, state.n};
+            kept.cut = listed.n <= LIST ? cut_among<JOIN_THREADS, true>(listed, whole, kept.weight, s, limit, low, high, kept.fraction)
+                                        : cut_among<JOIN_THREADS, true>(whole, whole, kept.weight, s, limit, low, high, kept.fraction);
+            // the kept members, to the sums of their parts
+            auto add = [&](float z, int j) {
+                const uint32_t k = order_key(z);
+                if (k >= low && k <= high) atomicAdd(&sums[(j + whole.lead) / (LOGITS_PART_PIECES * PER)], kept(z, j));
+            };
+            if (listed.n <= LIST)
+                listed.each_from(key_value(low), add);
+            else
+                whole.each_from(key_value(low), add);
+        }
+    } else {
+        if ((int)threadIdx.x < parts) {
+            const float z = m == INFINITY ? as_infinite(mine) : mine;
+            const double t = kept.weight.log2_of(z);
+            sums[threadIdx.x] = z > -INFINITY ? (u64)ldexp(in[threadIdx.x].sum * exp2_64<11>(t), kept.fraction) : 0;
+        }
+        if (draw.first) {  // (no histogram was asked for: the first of the largest)
+            int j = 0x7FFFFFFF;
+            whole.each([&](float z, int at) { j = min(j, z == best ? at : 0x7FFFFFFF); });
+            __syncthreads();
+            j = block_all<JOIN_THREADS>(j, reinterpret_cast<int *>(s.part32), [](int p, int q) { return p < q ? p : q; });
+            if (threadIdx.x == 0) {
+                a.classes[r] = j;
+                if (a.log_prob) a.log_prob[r] = 0.0f;
+            }
+            return;
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {  // the part
+        u64 total = 0;
+        for (int p = lane; p < parts; p += 64) total += sums[p];
+        total = wave_sum(total);
+        const u64 target = target_of(draw.u, total);
+        u64 before = 0;
+        for (int p = 0; p < parts; p += 64) {
+            const u64 own = p + lane < parts ? sums[p + lane] : 0, upto = before + wave_scan(own);
+            if (upto > target && upto - own <= target) chosen = p + lane, chosen_before = upto - own;
+            before = __shfl(upto, 63);
+        }
+        if (lane == 0) s.w[0] = total;
+    }
+    __syncthreads();
+    const u64 total = s.w[0], target = target_of(draw.u, total), before = chosen_before;
+    HeldRow<T, JOIN_ROUNDS> row = part_row<T, JOIN_ROUNDS>(a, r, chosen, JOIN_THREADS);
+    if (m == INFINITY) row.only_infinite();
+    u64 own[JOIN_ROUNDS];
+    const u64 here = CUT ? sum_values<JOIN_THREADS, true>(row, own, s.part64, kept.lowest(), kept) : sum_values<JOIN_THREADS, false>(row, own, s.part64, -INFINITY, kept);
+    if (here == 0) {  // (a part whose weights are all below the point by themselves, if not by their sum: its largest)
+        const float part_best = m == INFINITY ? 0.0f : in[chosen].best;
+        int j = 0x7FFFFFFF;
+        row.each([&](float z, int at) { j = min(j, z == part_best ? at : 0x7FFFFFFF); });
+        j = block_all<JOIN_THREADS>(j, reinterpret_cast<int *>(s.part32), [](int p, int q) { return p < q ? p : q; });
+        if (threadIdx.x == 0) write_answer(a, r, j, kept.weight.log2_of(part_best), kept.fraction, total);
+        return;
+    }
+    // (sums made in another way may differ by a rounding: the last of the part then)
+    first_beyond<JOIN_THREADS>(row, own, s.part64, min(target - before, here - 1), kept,
+                               [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
+}
+
+template <typename T>
+hipError_t launch(const SampleArgs &a, char *ws, hipStream_t s) {
+    if (held_rows(a.in))
+        return by_size(logits_pieces(a.in.n, a.in.bf16), [&](auto N, auto THREADS) {
+            return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { sample_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
+        });
+    const int parts = logits_parts(a.in.n, a.in.bf16);
+    const long most = rows_of_slice(a.in.n) < a.in.rows ? rows_of_slice(a.in.n) : a.in.rows;
+    SampleRow *rows = reinterpret_cast<SampleRow *>(ws);
+    SamplePart *sums = reinterpret_cast<SamplePart *>(ws + most * sizeof(SampleRow));
+    return by_slices(a.in.rows, most, [&](int r, int n) {
+        if (a.top_k || a.top_p || a.min_p) {
+            sample_part_kernel<T, true><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
+            sample_join_kernel<<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
+            sample_gather_kernel<T><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums, rows);
+            sample_finish_kernel<T, true><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
+        } else {
+            sample_part_kernel<T, false><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
+            sample_finish_kernel<T, false><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
+        }
+    });
+}
+
+}  // namespace
+
+size_t sample_part_bytes() { return sizeof(SamplePart); }
+size_t sample_row_bytes() { return sizeof(SampleRow); }
+
+hipError_t launch_sample(const SampleArgs &a, void *ws, hipStream_t s) { return a.in.bf16 ? launch<uint16_t>(a, static_cast<char *>(ws), s) : launch<float>(a, static_cast<char *>(ws), s); }
+
+}  // namespace sushi

@@ -1,0 +1,361 @@
+// The leading logits of a row and the probability mass outside them (logits.h).
+//
+// The row's groups (what a thread holds, or a 16-byte piece) have maxima; the k-th largest of these maxima is reached by k logits at
+// least, so what lies below it is not among the first k.  Little reaches it: 70 logits of 32001 with k = 64 and 512 groups.  Those are
+// listed in LDS, ranked, and the first k of them are the answer.  The mass outside is summed by itself, in 64 bits.
+// A list that is too long (many equal logits) is cut by histograms of the keys (row_order.h).
+#include "row_order.h"
+
+namespace sushi {
+
+namespace {
+
+constexpr int TOP_LIST = 2 * LOGITS_MAX_TOP;
+
+// A key that at least k of the keys reach (KEY_NONE + 1 if fewer are above that of -inf), close to the largest such.  By one wave, on
+// keys in LDS, `each` a lane.
+template <int EACH>
+__device__ uint32_t reached_by(const uint32_t *keys, int k) {
+    uint32_t own[EACH], low = 0xFFFFFFFFu, high = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        own[e] = keys[e * 64 + (threadIdx.x & 63)];
+        low = min(low, own[e]), high = max(high, own[e]);
+    }
+    auto count = [&](uint32_t key) {
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) n += __popcll(__ballot(own[e] >= key));
+        return n;
+    };
+    low = max(wave_all(low, [](uint32_t a, uint32_t b) { return a < b ? a : b; }), KEY_NONE + 1);
+    high = wave_all(high, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+    if (count(low) < k) return KEY_NONE + 1;
+    for (int i = 0; i < 20 && low < high; ++i) {
+        const uint32_t middle = low + (high - low) / 2 + 1;
+        const int n = count(middle);
+        if (n >= k) low = middle; else high = middle - 1;
+        if (n == k) break;
+    }
+    return low;
+}
+
+struct Order {
+    union {
+        u64 entry[TOP_LIST];  // keys above inverted indexes
+        uint32_t maxima[LOGITS_PART_PIECES];
+        SearchLds s;
+    };
+    int n;
+    uint32_t bound;
+};
+__device__ __forceinline__ u64 entry_of(uint32_t key, int j) { return (u64)key << 32 | (uint32_t)~j; }
+__device__ __forceinline__ uint32_t entry_key(u64 v) { return (uint32_t)(v >> 32); }
+
+// Ranks the list (n entries) and writes the first k as the row's answer; adds the others' weights to outside, theirs to inside.
+template <int THREADS>
+__device__ void write_first(const TopArgs &a, long r, Order &o, int n, const Weight &weight, bool infinite, double &inside, double &outside) {
+    auto put = [&](int rank, u64 v) {
+        const float z = key_value(entry_key(v));
+        const double w = exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
+        if (rank < a.k) {
+            a.values[r * a.k + rank] = z;
+            a.classes[r * a.k + rank] = (int)~(uint32_t)v;
+            inside += w;
+        } else {
+            outside += w;
+        }
+    };
+    if (n <= 256) {
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const u64 v = o.entry[i];
+            int rank = 0;
+            for (int e = 0; e < n; ++e) rank += o.entry[e] > v;
+            put(rank, v);
+        }
+    } else {
+        int size = 512;
+        while (size < n) size *= 2;
+        for (int i = n + threadIdx.x; i < size; i += THREADS) o.entry[i] = 0;
+        __syncthreads();
+        for (int width = 2; width <= size; width *= 2)
+            for (int d = width / 2; d > 0; d /= 2) {
+                for (int i = threadIdx.x; i < size / 2; i += THREADS) {
+                    const int lo = (i & ~(d - 1)) * 2 + (i & (d - 1)), hi = lo + d;
+                    const u64 p = o.entry[lo], q = o.entry[hi];
+                    if ((p < q) == ((lo & width) == 0)) o.entry[lo] = q, o.entry[hi] = p;
+                }
+                __syncthreads();
+            }
+        for (int i = threadIdx.x; i < n; i += THREADS) put(i, o.entry[i]);
+    }
+    for (int i = n + threadIdx.x; i < a.k; i += THREADS) a.values[r * a.k + i] = -INFINITY, a.classes[r * a.k + i] = -1;
+}
+
+// The list from a source with more than TOP_LIST logits that reach the bound: exactly the first k; the rest's weights as they are
+// below the cut, from the whole row.
+template <int THREADS, typename T>
+__device__ __noinline__ void list_exactly(const TopArgs &a, const Row<T> &row, Order &o, uint32_t low, int n, const Weight &weight, bool infinite, double *outside) {
+    __syncthreads();
+    if (threadIdx.x == 0) o.s.before = 0, o.s.weight_before = 0, o.s.inside = n, o.n = 0;
+    __syncthreads();
+    const Cut cut = cut_among<THREADS, false>(row, row, weight, o.s, Limit{(uint32_t)a.k, INFINITY}, low, 0xFF800000u, 0);
+    __syncthreads();  // (the entries lie where the search was)
+    double sum = 0.0;
+    row.each([&](float z, int j) {
+        const uint32_t k = order_key(z);
+        if (k != KEY_NONE && cut.keeps(k, j))
+            o.entry[min(atomicAdd(&o.n, 1), TOP_LIST - 1)] = entry_of(k, j);
+        else
+            sum += exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
+    });
+    *outside = sum;
+    __syncthreads();
+}
+
+template <typename T, int N, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS < 1024 ? 6 : 4) void top_held_kernel(TopArgs a, int row0) {
+    __shared__ Order o;
+    __shared__ double part[2][16];
+    const long r = (long)row0 + blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    HeldRow<T, N> row(a.in, r, wave, THREADS / 64, lane);
+    float m = -INFINITY;
+    row.each([&](float z, int) { m = fmaxf(m, z); });
+    o.maxima[threadIdx.x] = order_key(m);
+    if (threadIdx.x == 0) o.n = 0;
+    __syncthreads();
+    if (wave == 0) {
+        const uint32_t bound = reached_by<THREADS / 64>(o.maxima, a.k);
+        if (lane == 0) o.bound = bound;
+    }
+    uint32_t best = 0;
+#pragma unroll
+    for (int e = 0; e < THREADS / 64; ++e) best = max(best, o.maxima[e * 64 + lane]);
+    best = wave_all(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    __syncthreads();
+    const uint32_t bound = o.bound;
+    const bool infinite = key_value(best) == INFINITY;
+    const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
+    // what reaches the bound is listed and taken out of the row
+    const float z_low = key_value(bound);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < row.rounds) {
+            constexpr int PER = HeldRow<T, N>::PER;
+            float v[PER];
+            unpack<T>(row.raw[i], v);
+            bool some = false;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) some |= v[e] >= z_low;
+            if (some) {
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (v[e] >= z_low) {
+                        const int at = atomicAdd(&o.n, 1);
+                        if (at < TOP_LIST) o.entry[at] = entry_of(order_key(v[e]), row.index(i) + e);
+                        v[e] = -INFINITY;
+                    }
+                row.raw[i] = pack<T>(v);
+            }
+        }
+    __syncthreads();
+    double inside = 0.0, outside = 0.0;
+    const int n = o.n;
+    if (n > TOP_LIST) {
+        const Row<T> whole(a.in, r, wave, THREADS / 64, lane);
+        list_exactly<THREADS>(a, whole, o, bound, n, weight, infinite, &outside);
+    } else if (a.rest) {
+        if (infinite) row.only_infinite();
+        row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
+    }
+    write_first<THREADS>(a, r, o, min(o.n, TOP_LIST), weight, infinite, inside, outside);
+    if (!a.rest) return;
+    inside = wave_sum(inside), outside = wave_sum(outside);
+    if (lane == 0) part[0][wave] = inside, part[1][wave] = outside;
+    __syncthreads();
+    inside = sum_across<THREADS / 64>(part[0]), outside = sum_across<THREADS / 64>(part[1]);
+    if (threadIdx.x == 0) a.rest[r] = inside > 0.0 ? (float)(outside / (inside + outside)) : 0.0f;
+}
+
+// ------------------------------------------------------------------ a row in parts
+
+constexpr int PART_THREADS = 256, PART_ROUNDS = LOGITS_PART_PIECES / PART_THREADS, JOIN_THREADS = 1024;
+
+// What a part has of the first k: what reaches the k-th largest of its own pieces' maxima.
+struct TopPart {
+    double outside;  // weights of the rest, at the part's own maximum
+    uint32_t best;   // key of the maximum
+    uint32_t bound;  // k logits of the part reach it, if it has as many
+    int n;           // listed; more than TOP_LIST: the list is not complete
+    u64 entry[TOP_LIST];
+};
+
+template <typename T>
+__global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int row0, int parts, TopPart *out) {
+    __shared__ Order o;
+    __shared__ double part_d[PART_THREADS / 64];
+    const long r = (long)row0 + blockIdx.x / parts;
+    const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    HeldRow<T, PART_ROUNDS> row(a.in, r, wave, PART_THREADS / 64, lane, part * LOGITS_PART_PIECES, LOGITS_PART_PIECES);
+    constexpr int PER = HeldRow<T, PART_ROUNDS>::PER;
+    // groups of 8, 4, 2 pieces or 1 of a thread: three times as many as k, if there are
+    const int each = 3 * a.k <= PART_THREADS ? 8 : 3 * a.k <= 2 * PART_THREADS ? 4 : 3 * a.k <= 4 * PART_THREADS ? 2 : 1;
+    uint32_t best = KEY_NONE, group = KEY_NONE;
+#pragma unroll
+    for (int i = 0; i < PART_ROUNDS; ++i) {
+        float v[PER], m = -INFINITY;
+        unpack<T>(row.raw[i], v);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) m = fmaxf(m, v[e]);
+        if (i < row.rounds) group = max(group, order_key(m));
+        if ((i + 1) % each == 0) {
+            o.maxima[i / each * PART_THREADS + threadIdx.x] = group;
+            best = max(best, group), group = KEY_NONE;
+        }
+    }
+    if (threadIdx.x == 0) o.n = 0;
+    __syncthreads();
+    if (wave == 0) {
+        const uint32_t bound = each == 8   ? reached_by<PART_THREADS / 64>(o.maxima, a.k)
+                               : each == 4 ? reached_by<2 * PART_THREADS / 64>(o.maxima, a.k)
+                               : each == 2 ? reached_by<4 * PART_THREADS / 64>(o.maxima, a.k)
+                                           : reached_by<8 * PART_THREADS / 64>(o.maxima, a.k);
+        if (lane == 0) o.bound = bound;
+    }
+    best = wave_all(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    __shared__ uint32_t part_k[PART_THREADS / 64];
+    if (lane == 0) part_k[wave] = best;
+    __syncthreads();
+    best = across_waves<PART_THREADS / 64>(part_k, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    const float z_low = key_value(o.bound);
+    TopPart &mine = out[blockIdx.x];
+#pragma unroll
+    for (int i = 0; i < PART_ROUNDS; ++i)
+        if (i < row.rounds) {
+            float v[PER];
+            unpack<T>(row.raw[i], v);
+            bool some = false;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) some |= v[e] >= z_low;
+            if (some) {
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (v[e] >= z_low) {
+                        const int at = atomicAdd(&o.n, 1);
+                        if (at < TOP_LIST) mine.entry[at] = entry_of(order_key(v[e]), row.index(i) + e);
+                        v[e] = -INFINITY;
+                    }
+                row.raw[i] = pack<T>(v);
+            }
+        }
+    const bool infinite = key_value(best) == INFINITY;
+    if (infinite) row.only_infinite();
+    const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
+    double outside = 0.0;
+    row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
+    outside = block_sum<PART_THREADS>(outside, part_d);
+    if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.n = o.n;
+}
+
+// The logits that a row's parts have listed.
+struct PartLists {
+    const TopPart *parts;
+    int n;
+    template <typename F>
+    __device__ __forceinline__ void each_from(float z_low, F f) const {
+        const uint32_t low = order_key(z_low);
+        for (int p = threadIdx.x >> 6; p < n; p += JOIN_THREADS / 64)
+            for (int i = threadIdx.x & 63; i < parts[p].n; i += 64) {
+                const u64 v = parts[p].entry[i];
+                if (entry_key(v) >= low) f(key_value(entry_key(v)), (int)~(uint32_t)v);
+            }
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int row0, int parts, const TopPart *in) {
+    __shared__ Order o;
+    __shared__ uint32_t part_k[2][JOIN_THREADS / 64];
+    __shared__ int part_n[2][JOIN_THREADS / 64];
+    __shared__ double part_d[2][JOIN_THREADS / 64];
+    const long r = (long)row0 + blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    in += (long)blockIdx.x * parts;
+    uint32_t best = 0, bound = 0;
+    int n = 0, most = 0;
+    if ((int)threadIdx.x < parts) best = in[threadIdx.x].best, bound = in[threadIdx.x].bound, n = most = in[threadIdx.x].n;  // (129 parts at most)
+    auto larger = [](uint32_t p, uint32_t q) { return p > q ? p : q; };
+    auto more = [](int p, int q) { return p > q ? p : q; };
+    best = block_all<JOIN_THREADS>(best, part_k[0], larger);
+    bound = block_all<JOIN_THREADS>(bound, part_k[1], larger);  // (k logits of one part reach it)
+    most = block_all<JOIN_THREADS>(most, part_n[0], more);
+    n = block_sum<JOIN_THREADS>(n, part_n[1]);
+    const bool infinite = key_value(best) == INFINITY;
+    const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
+    double inside = 0.0, outside = 0.0;
+    const PartLists lists{in, parts};
+    if (most > TOP_LIST) {  // (a part with many equal logits)
+        const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
+        // (no logits are missing above the largest bound of an incomplete list, but which that is is not worth a search here)
+        uint32_t ordered = 0;
+        whole.each([&](float z, int) { ordered += z > -INFINITY; });
+        __syncthreads();
+        ordered = block_sum<JOIN_THREADS>(ordered, part_k[1]);
+        list_exactly<JOIN_THREADS>(a, whole, o, KEY_NONE + 1, (int)ordered, weight, infinite, &outside);
+        n = o.n;
+    } else {
+        if ((int)threadIdx.x < parts && in[threadIdx.x].outside > 0.0) {
+            const float z = key_value(in[threadIdx.x].best);
+            outside = in[threadIdx.x].outside * exp2_64<11>(weight.log2_of(infinite ? as_infinite(z) : z));
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) o.s.before = 0, o.s.weight_before = 0, o.s.inside = n, o.n = 0;
+        __syncthreads();
+        Cut cut = keep_all();
+        if (n > MEMBERS && n > a.k) {  // (ranking more costs more than a histogram)
+            const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
+            cut = cut_among<JOIN_THREADS, false>(lists, whole, weight, o.s, Limit{(uint32_t)a.k, INFINITY}, bound, best, 0);
+            __syncthreads();
+        }
+        lists.each_from(-3.4028234663852886e38f, [&](float z, int j) {
+            const uint32_t k = order_key(z);
+            if (cut.keeps(k, j))
+                o.entry[min(atomicAdd(&o.n, 1), TOP_LIST - 1)] = entry_of(k, j);
+            else
+                outside += exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
+        });
+        __syncthreads();
+        n = o.n;
+    }
+    write_first<JOIN_THREADS>(a, r, o, n, weight, infinite, inside, outside);
+    if (!a.rest) return;
+    inside = wave_sum(inside), outside = wave_sum(outside);
+    if (lane == 0) part_d[0][wave] = inside, part_d[1][wave] = outside;
+    __syncthreads();
+    inside = sum_across<JOIN_THREADS / 64>(part_d[0]), outside = sum_across<JOIN_THREADS / 64>(part_d[1]);
+    if (threadIdx.x == 0) a.rest[r] = inside > 0.0 ? (float)(outside / (inside + outside)) : 0.0f;
+}
+
+template <typename T>
+hipError_t launch(const TopArgs &a, TopPart *ws, hipStream_t s) {
+    if (held_rows(a.in))
+        return by_size(logits_pieces(a.in.n, a.in.bf16), [&](auto N, auto THREADS) {
+            return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { top_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
+        });
+    const int parts = logits_parts(a.in.n, a.in.bf16);
+    return by_slices(a.in.rows, rows_of_slice(a.in.n), [&](int r, int n) {
+        top_part_kernel<T><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, ws);
+        top_join_kernel<T><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, ws);
+    });
+}
+
+}  // namespace
+
+size_t top_logits_part_bytes() { return sizeof(TopPart); }
+
+hipError_t launch_top_logits(const TopArgs &a, void *ws, hipStream_t s) {
+    return a.in.bf16 ? launch<uint16_t>(a, static_cast<TopPart *>(ws), s) : launch<float>(a, static_cast<TopPart *>(ws), s);
+}
+
+}  // namespace sushi
