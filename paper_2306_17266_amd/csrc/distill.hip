@@ -154,7 +154,7 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, floa
     if (a.loss) {
         double loss = 0.0;
         if (entries) {
-            const double log_sum = log(sum), log_list = log1p(-mass) - log(list_sum);
+            const double log_sum = log2_64(sum) * LN2, log_list = (log2_64(1.0 - mass) - log2_64(list_sum)) * LN2;
 #pragma unroll
             for (int o = 0; o < OWN; ++o)
                 if (own.counts[o]) {
@@ -164,7 +164,7 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, floa
                     if (p != 0.0) loss += p * (log_p - (student.log2_of(own.z[o]) * LN2 - log_sum));
                 }
             loss = wave_sum(loss);
-            if (wave == 0 && mass != 0.0) loss += mass * (log(mass) - (log(rest) - log_sum));
+            if (wave == 0 && mass != 0.0) loss += mass * ((log2_64(mass) - log2_64(rest)) * LN2 + log_sum);
         }
         if (a.k > 64) {
             if ((threadIdx.x & 63) == 0) part[3][wave] = loss;

@@ -42,6 +42,15 @@ __device__ __forceinline__ double exp2_64(double t) {
     return ldexp(fma(p, f, 1.0), (int)i);
 }
 
+// log2 in 64 bits, off by 1e-13 at most: the 32-bit one, and what its result lacks by two terms of the series of log(1 + d).
+__device__ __forceinline__ double log2_64(double x) {
+    const double m = __builtin_amdgcn_frexp_mant(x);
+    const float y = __builtin_amdgcn_logf((float)m);
+    const double d = fma(m, exp2_64<11>(-(double)y), -1.0);
+    const double r = (double)__builtin_amdgcn_frexp_exp(x) + ((double)y + d * fma(d, -0.5, 1.0) * 1.4426950408889634074);
+    return x > 0.0 ? r : x == 0.0 ? -INFINITY : NAN;
+}
+
 // Weights of a row's logits at a temperature: 2^log2_of().  An infinite maximum is no case of its own here: its row is read as
 // Row::only_infinite() says.
 struct Weight {

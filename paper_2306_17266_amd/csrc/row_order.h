@@ -1,8 +1,8 @@
 // What sampling (sample.hip) and the top logits (top_logits.hip) share: the last kept position of a row's order.
 //
 // Both need it: the first position at which the number of logits reaches k or (sampling) their summed weight reaches top_p of the
-// row's sum.  No row is sorted for it.  What lies in a range of keys that holds the position is ranked by comparing each with
-// each if it is little, and cut finer by histograms over the keys if it is not, until little or one key is left.
+// row's sum.  No row is sorted for it.  The range of keys that holds the position is cut finer by histograms over the keys until
+// a wave can rank what is left, or one key is left.
 //
 // Sums of weights are whole numbers (fixed point in 64 bits): the same in whatever order atomics in LDS make them, so that a class
 // whose interval of the sum is hit by the random number is the same in every run.  Which class that is is decided next to borders,
@@ -17,20 +17,12 @@ typedef unsigned long long u64;
 
 constexpr int BINS = 1024;
 constexpr double LN2 = 6.931471805599453094e-01;
-constexpr int MEMBERS = 512;  // that are ranked by comparing each with each
+constexpr int MEMBERS = 64;  // that one wave ranks, a lane each
 
 struct SearchLds {
-    union {
-        struct {
-            u64 weight[BINS + 1];  // (the last: of what is in no order)
-            uint32_t count[BINS];
-        };
-        struct {  // members of the range that is cut no further
-            u64 w[MEMBERS], w_upto[MEMBERS];
-            uint32_t key[MEMBERS], n_upto[MEMBERS];
-            int index[MEMBERS];
-        };
-    };
+    u64 weight[BINS + 1];  // (the last: of what is in no order)
+    uint32_t count[BINS];
+    u64 member[MEMBERS];  // keys above indexes
     u64 part64[16];
     uint32_t part32[16];
     float part_f[16];
@@ -52,11 +44,7 @@ __device__ __forceinline__ Cut keep_all() { return Cut{KEY_NONE + 1, 0x7FFFFFFF}
 __device__ __forceinline__ u64 fixed_weight(double t, int fraction) {
     return (u64)__double_as_longlong(ldexp(exp2_64<11>(t), fraction) + 4503599627370496.0) & ((1ull << 52) - 1);
 }
-__host__ __device__ inline int bits_of(int n) {  // n <= 2^bits_of(n)
-    int lg = 0;
-    while ((1 << lg) < n) ++lg;
-    return lg;
-}
+__device__ __forceinline__ int bits_of(int n) { return n > 1 ? 32 - __builtin_clz(n - 1) : 0; }  // n <= 2^bits_of(n)
 // Bits behind the point for sums of n weights: below 2^63.
 __device__ __forceinline__ int fraction_bits(int n) { return min(62 - bits_of(n), 50); }
 
@@ -68,9 +56,10 @@ struct Limit {
 };
 
 // Finds the interval in which the limit is reached, counting from (s.before, s.weight_before); s.bin = -1: in none.  n, w: this
-// thread's run of intervals, their members and weights.  share >= 0: that share of all weights is the limit's.
+// thread's run of intervals, their members and weights.  share >= 0: that share of all weights is the limit's.  From interval `stop` on the
+// limit counts as reached.
 template <int THREADS>
-__device__ void find_bin(SearchLds &s, Limit &limit, float share, const uint32_t (&n)[BINS / THREADS], const u64 (&w)[BINS / THREADS]) {
+__device__ void find_bin(SearchLds &s, Limit &limit, float share, const uint32_t (&n)[BINS / THREADS], const u64 (&w)[BINS / THREADS], int stop = BINS) {
     constexpr int OWN = BINS / THREADS, WAVES = THREADS / 64;
     const int tid = threadIdx.x, wave = tid >> 6;
     uint32_t n_before = s.before, n_own = 0;
@@ -85,16 +74,13 @@ __device__ void find_bin(SearchLds &s, Limit &limit, float share, const uint32_t
     n_before += sum_before<WAVES>(s.part32) + n_upto - n_own;
     w_before += sum_before<WAVES>(s.part64) + w_upto - w_own;
     if (share >= 0.0f) limit.weight = fmax((double)share * (double)sum_across<WAVES>(s.part64), 1.0);
-    if (!limit.reached(n_before, w_before) && limit.reached(n_before + n_own, w_before + w_own)) {  // (one thread at most)
-        bool found = false;
+    bool reached = limit.reached(n_before, w_before) || tid * OWN > stop;
 #pragma unroll
-        for (int b = 0; b < OWN; ++b) {
-            if (!found && limit.reached(n_before + n[b], w_before + w[b])) {
-                found = true;
-                s.bin = tid * OWN + b, s.before = n_before, s.weight_before = w_before, s.inside = n[b];
-            }
-            n_before += n[b], w_before += w[b];
-        }
+    for (int b = 0; b < OWN; ++b) {
+        const bool now = limit.reached(n_before + n[b], w_before + w[b]) || tid * OWN + b >= stop;
+        if (now && !reached) s.bin = tid * OWN + b, s.before = n_before, s.weight_before = w_before, s.inside = n[b];  // (once at most)
+        reached = now;
+        n_before += n[b], w_before += w[b];
     }
     __syncthreads();
 }
@@ -123,6 +109,7 @@ __device__ void find_equal(const Row<T> &row, SearchLds &s, uint32_t key, u64 ta
     row.each_from(z_low, [&](float z, int) { sum += order_key(z) == key; });
     sum = wave_sum(sum);
     __syncthreads();
+    if (threadIdx.x == 0) s.rank = 0x7FFFFFFF;  // (if there are fewer)
     if ((threadIdx.x & 63) == 0) s.part64[threadIdx.x >> 6] = sum;
     __syncthreads();
     u64 before = sum_before<THREADS / 64>(s.part64);
@@ -158,12 +145,11 @@ __device__ __forceinline__ Cut cut_among(const R &source, const Row<T> &row, con
                 while (m < need && !limit.reached(s.before, s.weight_before + m * w)) ++m;
                 need = m < need ? m : need;
             }
-            if (need > s.inside) need = s.inside;
             find_equal<THREADS>(row, s, low, need - 1);
             return Cut{low, s.rank};
         }
-        int shift = 0;
-        while ((high - low) >> shift >= (uint32_t)BINS) ++shift;
+        const uint32_t spread = (high - low) / BINS;
+        const int shift = spread ? 32 - __builtin_clz(spread) : 0;  // (the smallest with less than BINS intervals)
         __syncthreads();
         for (int b = threadIdx.x; b < BINS; b += THREADS) s.count[b] = 0, s.weight[b] = 0;
         __syncthreads();
@@ -184,47 +170,32 @@ __device__ __forceinline__ Cut cut_among(const R &source, const Row<T> &row, con
         if ((high - low) >> shift > 0) low = high - ((1u << shift) - 1);
     }
     __syncthreads();
-    if (threadIdx.x == 0) s.n = 0, s.rank = MEMBERS;
-    for (int i = threadIdx.x; i < MEMBERS; i += THREADS) s.n_upto[i] = 0, s.w_upto[i] = 0;
+    if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
     source.each_from(key_value(low), [&](float z, int j) {
         const uint32_t k = order_key(z);
-        if (k <= high) {
-            const int at = min(atomicAdd(&s.n, 1), MEMBERS - 1);
-            s.key[at] = k, s.index[at] = j;
-            if (BY_WEIGHT) s.w[at] = weigh(z);
-        }
+        if (k <= high) s.member[min(atomicAdd(&s.n, 1), MEMBERS - 1)] = (u64)k << 32 | (uint32_t)~j;
     });
     __syncthreads();
-    // each member with each: several threads share a member
-    const int n = min(s.n, MEMBERS);
-    int padded = 64;
-    while (padded < n) padded *= 2;
-    const int sharing = max(THREADS / padded, 1);
-    for (int at = threadIdx.x; at < padded * sharing; at += THREADS) {
-        const int i = at & (padded - 1), first = at / padded;
-        if (i < n) {
-            const uint32_t k = s.key[i];
-            const int j = s.index[i];
-            uint32_t upto = 0;
-            u64 w = 0;
-            for (int o = first; o < n; o += sharing)
-                if (s.key[o] > k || (s.key[o] == k && s.index[o] <= j)) {
-                    ++upto;
-                    if (BY_WEIGHT) w += s.w[o];
-                }
-            atomicAdd(&s.n_upto[i], upto);
-            if (BY_WEIGHT) atomicAdd(&s.w_upto[i], w);
+    if (threadIdx.x < 64) {
+        const int n = min(s.n, MEMBERS);
+        const u64 own = (int)threadIdx.x < n ? s.member[threadIdx.x] : 0;
+        const u64 w = BY_WEIGHT && own ? weigh(key_value((uint32_t)(own >> 32))) : 0;
+        uint32_t n_upto = 0;
+        u64 w_upto = 0;
+        for (int o = 0; o < n; ++o) {
+            const bool upto = read_lane(own, o) >= own;
+            n_upto += upto;
+            if (BY_WEIGHT) w_upto += upto ? read_lane(w, o) : 0;
         }
+        // the first that reaches the limit, or the last (weights of a range and of its members differ by roundings)
+        const bool reached = own && (n_upto == (uint32_t)n || limit.reached(s.before + n_upto, s.weight_before + w_upto));
+        const uint32_t rank = wave_all(reached ? n_upto : 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+        if (reached && n_upto == rank) s.member[0] = own;
+        if (n == 0 && threadIdx.x == 0) s.member[0] = (u64)high << 32;  // (nothing there: what is above, and no index)
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS)
-        if ((int)s.n_upto[i] == n || limit.reached(s.before + s.n_upto[i], s.weight_before + s.w_upto[i])) atomicMin(&s.rank, (int)s.n_upto[i]);
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS)
-        if ((int)s.n_upto[i] == s.rank) s.bin = i;
-    __syncthreads();
-    return Cut{s.key[s.bin], s.index[s.bin]};
+    return Cut{(uint32_t)(s.member[0] >> 32), (int)~(uint32_t)s.member[0]};
 }
 
 // The maximum of a row; NaN is none.

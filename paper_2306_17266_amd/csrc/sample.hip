@@ -21,11 +21,11 @@ struct Grid {
     }
     __device__ __forceinline__ Grid(float best, double inv_t, double anchor_) : anchor(anchor_), scale(inv_t * (1.4426950408889634074 * BINS_PER_LOG2)) { top = floor(place(best)); }
     // Key of the smallest logit in intervals 0 .. b.
-    __device__ uint32_t lowest_key(int b, float best) const {
+    __device__ __forceinline__ uint32_t lowest_key(int b, float best, double unit) const {  // unit: 1 / scale, about
         const uint32_t lowest = KEY_NONE + 1, highest = order_key(best);
         const double x = top + (b + 1.0);
         if (b >= BINS - 1 || !(scale > 0.0)) return lowest;
-        uint32_t k = order_key((float)fmin(fmax(anchor - x / scale, -3.4028234663852886e38), 3.4028234663852886e38));
+        uint32_t k = order_key((float)fmin(fmax(anchor - x * unit, -3.4028234663852886e38), 3.4028234663852886e38));
         while (k > lowest && place(key_value(k - 1)) < x) --k;
         while (k < highest && place(key_value(k)) >= x) ++k;
         return k;
@@ -52,8 +52,8 @@ struct Packed {
     }
     __device__ __forceinline__ uint32_t count(u64 v) const { return (uint32_t)(v >> count_at); }
     __device__ __forceinline__ u64 lack(u64 v) const { return v & ((1ull << count_at) - 1); }
-    // Weight of count members of which so much is lacking of the weight 2^t each.
-    __device__ __forceinline__ double weight(uint32_t count, u64 lacking, double t) const { return ((double)count - ldexp((double)lacking, -fraction)) * exp2_64<11>(t); }
+    // Weight of an interval's members, relative to its upper end.
+    __device__ __forceinline__ double sum(uint32_t count, u64 lacking) const { return (double)count - ldexp((double)lacking, -fraction); }
 };
 
 // The histogram of what a source holds, in s.weight.
@@ -67,30 +67,6 @@ __device__ void build_histogram(const R &row, const Grid &grid, const Packed &pa
         atomicAdd(&s.weight[z > -INFINITY ? b : BINS], packed.one(t - g));  // (no branch: it would be one for each logit)
     });
     __syncthreads();
-}
-
-// The keys of the interval in which the limit is reached; low > high: in none.  share >= 0: that share of the row's sum is the limit's
-// weight.  count, lacking: this thread's run of intervals.  equal: members of the first that equal the maximum and are in neither.
-struct Range {
-    uint32_t low, high;
-};
-template <int THREADS>
-__device__ Range search(SearchLds &s, const Grid &grid, const Packed &packed, float best, Limit &limit, float share, uint32_t (&count)[BINS / THREADS],
-                        const u64 (&lacking)[BINS / THREADS], uint32_t equal, int fraction) {
-    constexpr int OWN = BINS / THREADS;
-    const double above = grid.place(best) - grid.top;  // of the maximum within its interval
-    u64 w[OWN];
-#pragma unroll
-    for (int i = 0; i < OWN; ++i) {
-        const int b = threadIdx.x * OWN + i;
-        double wd = count[i] && b < BINS - 1 ? packed.weight(count[i], lacking[i], (above - b) * (1.0 / BINS_PER_LOG2)) : 0.0;
-        if (b == 0) count[i] += equal, wd += equal;
-        w[i] = (u64)ldexp(wd, fraction);
-    }
-    find_bin<THREADS>(s, limit, share, count, w);
-    const int bin = s.bin;
-    if (bin < 0) return Range{1, 0};
-    return Range{grid.lowest_key(bin, best), bin > 0 ? grid.lowest_key(bin - 1, best) - 1 : 0xFFFFFFFFu};
 }
 
 // How a row is drawn from.
@@ -107,10 +83,48 @@ struct Draw {
         first = !(temperature > 0.0f);
         if (first) temperature = 1.0f, k = 1, top_p = 1.0f, min_p = 0.0f;
     }
-    __device__ __forceinline__ bool cuts(int n) const { return k < n || top_p < 1.0f; }
+    __device__ __forceinline__ bool cuts(int n) const { return k < n || top_p < 1.0f || min_p > 0.0f; }
     __device__ __forceinline__ float share() const { return top_p < 1.0f ? fmaxf(top_p, 0.0f) : -1.0f; }
-    __device__ __forceinline__ double t_min() const { return min_p > 0.0f ? log2((double)min_p) : -INFINITY; }
+    __device__ __forceinline__ double t_min() const { return min_p > 0.0f ? log2_64((double)min_p) : -INFINITY; }
 };
+
+// Where a row is cut: interval `start` of the grid (none: BINS), and the keys in question.  All above them are kept, none below.
+struct Range {
+    int start;
+    uint32_t low, high;
+};
+// count, lacking: this thread's run of intervals.  equal: members of the first that equal the maximum and are in neither.  t_min: log2
+// of the weight from which min_p keeps.  s.before, s.weight_before: zero.
+template <int THREADS>
+__device__ Range search(SearchLds &s, const Grid &grid, const Packed &packed, float best, Limit &limit, const Draw &draw, double t_min, uint32_t (&count)[BINS / THREADS],
+                        const u64 (&lacking)[BINS / THREADS], uint32_t equal, int fraction) {
+    constexpr int OWN = BINS / THREADS;
+    const double above = grid.place(best) - grid.top;  // of the maximum within its interval
+    u64 w[OWN];
+    double edge = exp2_64<11>((above - (int)threadIdx.x * OWN) * (1.0 / BINS_PER_LOG2));  // weight of an interval's upper end
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int b = threadIdx.x * OWN + i;
+        double wd = b < BINS - 1 ? packed.sum(count[i], lacking[i]) * edge : 0.0;
+        edge *= 9.438743126816934966e-01;  // 2^(-1/12)
+        if (b == 0) count[i] += equal, wd += equal;
+        w[i] = (u64)ldexp(wd, fraction);
+    }
+    // the interval of min_p's border; the next one too where the border lies next to it
+    const double border = above - t_min * BINS_PER_LOG2;
+    const int stop = (int)fmin(fmax(border - 1e-6, 0.0), (double)BINS), stop_end = (int)fmin(border + 1e-6, (double)BINS);
+    find_bin<THREADS>(s, limit, draw.share(), count, w, stop);
+    const int bin = s.bin;
+    if (bin < 0) return Range{BINS, 1, 0};
+    const int end = bin == stop ? max(stop_end, bin) : bin;
+    const double unit = (double)draw.temperature * (LN2 / BINS_PER_LOG2);
+    // (the lower and the upper end, in neighbouring lanes)
+    const uint32_t k = grid.lowest_key(threadIdx.x & 1 ? bin - 1 : end, best, unit);
+    const uint32_t low = read_lane(k, 0), above_high = read_lane(k, 1);
+    if (end != bin && threadIdx.x == 0) s.inside = 0x7FFFFFFF;  // (more than is known)
+    __syncthreads();
+    return Range{bin, low, bin > 0 ? above_high - 1 : 0xFFFFFFFFu};
+}
 
 // Which logits are kept, and their weights.
 struct Kept {
@@ -122,19 +136,13 @@ struct Kept {
         const double t = weight.log2_of(z);
         return cut.keeps(order_key(z), j) && t >= t_min ? fixed_weight(t, fraction) : 0;
     }
-    // What is below has no weight (min_p's border a little lowered: the exact test is above).
-    __device__ __forceinline__ float lowest() const {
-        double z = weight.best + t_min / weight.scale;
-        z -= fabs(z) * 1e-6;
-        return fmaxf(key_value(cut.key), z > -3e38 && z < 3e38 ? (float)z : -INFINITY);
-    }
 };
 
 __device__ __forceinline__ u64 target_of(float u, u64 total) { return min((u64)((double)u * (double)total), total - 1); }
 
 __device__ __forceinline__ void write_answer(const SampleArgs &a, long r, int j, double log2_of, int fraction, u64 total) {
     a.classes[r] = j;
-    if (a.log_prob) a.log_prob[r] = (float)((log2_of + fraction - log2((double)total)) * LN2);
+    if (a.log_prob) a.log_prob[r] = (float)((log2_of + fraction - log2_64((double)total)) * LN2);
 }
 __device__ __forceinline__ void write_nothing(const SampleArgs &a, long r) {  // (nothing to draw from)
     a.classes[r] = -1;
@@ -207,6 +215,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
     const bool infinite = best == INFINITY;
     if (infinite) row.only_infinite(), best = 0.0f;
     Kept kept{Weight(best, inv_t), keep_all(), draw.t_min(), fraction_bits(a.in.n)};
+    bool few = false;
     if (draw.cuts(a.in.n)) {
         constexpr int OWN = BINS / THREADS;
         const Grid grid(best, inv_t, best);  // (the largest logit is place 0: a row of equal logits has exact sums, and its cut is where the count says)
@@ -221,18 +230,16 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
             count[i] = packed.count(v), lacking[i] = packed.lack(v);
         }
         Limit limit{(uint32_t)draw.k, INFINITY};
-        const Range f = search<THREADS>(s, grid, packed, best, limit, draw.share(), count, lacking, 0, kept.fraction);
-        if (f.low <= f.high) {
+        const Range f = search<THREADS>(s, grid, packed, best, limit, draw, kept.t_min, count, lacking, 0, kept.fraction);
+        if (f.start < BINS) {
             Row<T> whole(a.in, r, wave, THREADS / 64, lane);
             if (infinite) whole.only_infinite();
             kept.cut = cut_among<THREADS, true>(row, whole, kept.weight, s, limit, f.low, f.high, kept.fraction);
-            __syncthreads();
+            few = s.before <= (uint32_t)a.in.n / 64;
         }
     }
     u64 own[N];
-    const u64 total = draw.cuts(a.in.n) || draw.min_p > 0.0f
-                          ? sum_values<THREADS, true>(row, own, s.part64, kept.lowest(), kept)
-                          : sum_values<THREADS, false>(row, own, s.part64, -INFINITY, [&](float z, int) { return fixed_weight(kept.weight.log2_of(z), kept.fraction); });
+    const u64 total = few ? sum_values<THREADS, true>(row, own, s.part64, key_value(kept.cut.key), kept) : sum_values<THREADS, false>(row, own, s.part64, -INFINITY, kept);
     first_beyond<THREADS>(row, own, s.part64, target_of(draw.u, total), kept, [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
 }
 
@@ -255,7 +262,8 @@ struct SamplePart {
 // What the parts need to know of their row once the histograms are joined.
 struct SampleRow {
     float best;
-    uint32_t low, high;  // the interval in which the row is cut (low > high: none)
+    int start;           // the interval in which the row is cut (Range)
+    uint32_t low, high;
     uint32_t before, inside;
     u64 weight_before;
     double limit;
@@ -311,15 +319,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a,
     __shared__ SearchLds s;
     __shared__ double top[MOST_PARTS];
     __shared__ float maxima[MOST_PARTS];
+    __shared__ uint32_t n_equal[MOST_PARTS], n_ordered[MOST_PARTS];
     static_assert(BINS == JOIN_THREADS, "a thread has one interval");
     const long r = (long)row0 + blockIdx.x;
     in += (long)blockIdx.x * parts;
     SampleRow &row = out[blockIdx.x];
     const Draw draw(a, r);
     float m = -INFINITY;
-    if ((int)threadIdx.x < parts) m = maxima[threadIdx.x] = in[threadIdx.x].best, top[threadIdx.x] = in[threadIdx.x].top;
+    if ((int)threadIdx.x < parts) {
+        const SamplePart &p = in[threadIdx.x];
+        m = maxima[threadIdx.x] = p.best, top[threadIdx.x] = p.top, n_equal[threadIdx.x] = p.equal, n_ordered[threadIdx.x] = p.ordered;
+    }
+    s.count[threadIdx.x] = 0, s.weight[threadIdx.x] = 0;
     m = block_all<JOIN_THREADS>(m, s.part_f, [](float p, float q) { return fmaxf(p, q); });
-    if (threadIdx.x == 0) row.best = m, row.n = 0, row.low = 1, row.high = 0, s.before = 0, s.weight_before = 0;
+    if (threadIdx.x == 0) row.best = m, row.n = 0, row.start = BINS, s.before = 0, s.weight_before = 0;
     if (m == -INFINITY || !draw.cuts(a.in.n)) return;
     const float best = m == INFINITY ? 0.0f : m;
     const int fraction = fraction_bits(a.in.n);
@@ -328,80 +341,106 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a,
     __syncthreads();
     uint32_t count[1] = {0}, equal = 0, ordered = 0;
     u64 lacking[1] = {0};
-    for (int p = 0; p < parts; ++p) {
-        if (maxima[p] == -INFINITY || (m == INFINITY && maxima[p] < INFINITY)) continue;
-        // the part's intervals lie `down` further down
-        const int down = (int)fmin(top[p] - grid.top, (double)BINS), b = (int)threadIdx.x - down;
-        ordered += in[p].ordered;
-        if (maxima[p] == m) equal += in[p].equal;
-        if (b >= 0 && threadIdx.x < BINS - 1) {
-            const u64 v = in[p].weight[b];
-            count[0] += packed.count(v), lacking[0] += packed.lack(v);
-            if (b == 0 && maxima[p] < m) {  // what equals the part's maximum, at its own place
+    constexpr int BATCH = 8;  // (their loads are on the way together)
+    for (int first = 0; first < parts; first += BATCH) {
+        u64 v[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) v[i] = in[min(first + i, parts - 1)].weight[threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int p = first + i;
+            if (p >= parts || maxima[p] == -INFINITY || (m == INFINITY && maxima[p] < INFINITY)) continue;
+            ordered += n_ordered[p];
+            if (maxima[p] == m) equal += n_equal[p];
+            // the part's intervals lie `down` further down
+            const int down = (int)fmin(top[p] - grid.top, (double)BINS), to = (int)threadIdx.x + down;
+            if (down == 0 && threadIdx.x < BINS - 1) {
+                count[0] += packed.count(v[i]), lacking[0] += packed.lack(v[i]);
+            } else if (to < BINS - 1 && v[i]) {
+                atomicAdd(&s.count[to], packed.count(v[i]));
+                atomicAdd(&s.weight[to], packed.lack(v[i]));
+            }
+            if (threadIdx.x == 0 && maxima[p] < m && down < BINS - 1) {  // what equals the part's maximum, at its own place
                 const double t = grid.place(maxima[p]);
-                count[0] += in[p].equal, lacking[0] += in[p].equal * packed.lack(packed.one(t - floor(t)));
+                atomicAdd(&s.count[down], n_equal[p]);
+                atomicAdd(&s.weight[down], n_equal[p] * packed.lack(packed.one(t - floor(t))));
             }
         }
     }
+    __syncthreads();
+    count[0] += s.count[threadIdx.x], lacking[0] += s.weight[threadIdx.x];
     // what falls off the end, in the last interval
-    const uint32_t placed = block_sum<JOIN_THREADS>(count[0], s.part32);
+    const uint32_t placed = block_sum<JOIN_THREADS>(threadIdx.x < BINS - 1 ? count[0] : 0u, s.part32);
     if (threadIdx.x == BINS - 1) count[0] = ordered - placed - equal;
     __syncthreads();
     Limit limit{(uint32_t)draw.k, INFINITY};
-    const Range f = search<JOIN_THREADS>(s, grid, packed, best, limit, draw.share(), count, lacking, equal, fraction);
-    if (threadIdx.x == 0)
-        row.low = f.low, row.high = f.high, row.before = s.before, row.inside = s.inside, row.weight_before = s.weight_before, row.limit = limit.weight;
+    const Range f = search<JOIN_THREADS>(s, grid, packed, best, limit, draw, draw.t_min(), count, lacking, equal, fraction);
+    if (threadIdx.x == 0) {
+        row.start = f.start, row.low = f.low, row.high = f.high;
+        row.before = s.before, row.inside = s.inside, row.weight_before = s.weight_before, row.limit = limit.weight;
+    }
 }
 
-// Third launch: each part lists its members of that interval, and sums what is kept above it.
+// Third launch: each part lists its members of that interval, and sums the weights above it (from its histogram).
 template <typename T>
 __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs a, int row0, int parts, SamplePart *part_out, SampleRow *rows) {
-    __shared__ u64 part64[PART_THREADS / 64];
+    __shared__ double part_d[PART_THREADS / 64];
     __shared__ int n, at;
+    constexpr int OWN = BINS / PART_THREADS;
     const long r = (long)row0 + blockIdx.x / parts;
     SampleRow &state = rows[blockIdx.x / parts];
     SamplePart &mine = part_out[blockIdx.x];
-    const float m = state.best;
+    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
+    u64 v[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) v[i] = mine.weight[i * PART_THREADS + threadIdx.x];
+    const float m = state.best, part_best = mine.best;
     const uint32_t low = state.low, high = state.high;
+    const int start = state.start;
     const Draw draw(a, r);
-    const bool cut = low <= high;
-    Kept kept{Weight(m == INFINITY ? 0.0f : m, 1.0 / (double)draw.temperature), cut ? Cut{high, -1} : keep_all(), draw.t_min(), fraction_bits(a.in.n)};
-    const float z_low = cut ? key_value(low) : kept.lowest();
-    const float own = m == INFINITY ? (mine.best == INFINITY ? 0.0f : -INFINITY) : mine.best;
-    if (m == -INFINITY || !(own >= z_low)) {  // (nothing here)
+    if (part_best == -INFINITY || (m == INFINITY && part_best < INFINITY)) {  // (nothing here)
         if (threadIdx.x == 0) mine.kept = 0;
         return;
     }
-    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
     if (m == INFINITY) row.only_infinite();
+    const float best = m == INFINITY ? 0.0f : m, own_best = part_best == INFINITY ? 0.0f : part_best;
+    const double inv_t = 1.0 / (double)draw.temperature;
+    const Grid grid(best, inv_t, 0.0);
+    const Packed packed(LOGITS_PART_PIECES * HeldRow<T, PART_ROUNDS>::PER);
+    const int fraction = fraction_bits(a.in.n);
     if (threadIdx.x == 0) n = 0;
-    __syncthreads();
-    u64 sum = 0;
+    // weights of the part's intervals before the row's `start`
+    const double down = mine.top - grid.top, above = grid.place(best) - grid.top;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int b = i * PART_THREADS + threadIdx.x;
+        if (v[i] && b < BINS - 1 && b + down < start)
+            sum += packed.sum(packed.count(v[i]), packed.lack(v[i])) * exp2_64<11>((above - down - b) * (1.0 / BINS_PER_LOG2));
+    }
+    if (threadIdx.x == 0 && down < start) sum += mine.equal * exp2_64<11>(Weight(best, inv_t).log2_of(own_best));
+    sum = block_sum<PART_THREADS>(sum, part_d);
+    if (threadIdx.x == 0) mine.kept = (u64)ldexp(sum, fraction);
+    if (start >= BINS || !(own_best >= key_value(low))) return;
     int members = 0;
-    row.each_from(z_low, [&](float z, int j) {
+    row.each([&](float z, int) {
         const uint32_t k = order_key(z);
-        sum += kept(z, j);
-        members += cut && k >= low && k <= high;
+        members += k >= low && k <= high;
     });
-    // a run of the row's list for this part's members
+    // a run of the row's list for them
     int before = wave_scan(members);
     const int all = __shfl(before, 63), lane = threadIdx.x & 63;
     int wave_at = 0;
     if (lane == 0 && all) wave_at = atomicAdd(&n, all);
     before += __shfl(wave_at, 0) - members;
-    sum = wave_sum(sum);
-    if (lane == 0) part64[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        if (n) at = atomicAdd(&state.n, n);
-        mine.kept = part64[0] + part64[1] + part64[2] + part64[3];
-    }
+    if (threadIdx.x == 0 && n) at = atomicAdd(&state.n, n);
     __syncthreads();
     before += at;
     if (members)
-        row.each_from(z_low, [&](float z, int j) {
+        row.each_from(key_value(low), [&](float z, int j) {
             const uint32_t k = order_key(z);
-            if (cut && k >= low && k <= high) {
+            if (k <= high) {
                 if (before < LIST) state.entry[before] = (u64)k << 32 | (uint32_t)j;
                 ++before;
             }
@@ -426,7 +465,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
     __shared__ SearchLds s;
     __shared__ u64 sums[MOST_PARTS];
     __shared__ int chosen;
-    __shared__ u64 chosen_before;
+    __shared__ u64 chosen_before, all_parts;
     constexpr int PER = 16 / sizeof(T);
     const long r = (long)row0 + blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -447,10 +486,11 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
     if (CUT) {
         const SampleRow &state = rows[blockIdx.x];
         const uint32_t low = state.low, high = state.high;
+        const int start = state.start;
         if (threadIdx.x == 0) s.before = state.before, s.weight_before = state.weight_before, s.inside = state.inside;
         if ((int)threadIdx.x < parts) sums[threadIdx.x] = in[threadIdx.x].kept;
         __syncthreads();
-        if (low <= high) {
+        if (start < BINS) {
             const Limit limit{(uint32_t)draw.k, state.limit};
             const Listed listed{state.entry, state.n};
             kept.cut = listed.n <= LIST ? cut_among<JOIN_THREADS, true>(listed, whole, kept.weight, s, limit, low, high, kept.fraction)
@@ -495,14 +535,14 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
             if (upto > target && upto - own <= target) chosen = p + lane, chosen_before = upto - own;
             before = __shfl(upto, 63);
         }
-        if (lane == 0) s.w[0] = total;
+        if (lane == 0) all_parts = total;
     }
     __syncthreads();
-    const u64 total = s.w[0], target = target_of(draw.u, total), before = chosen_before;
+    const u64 total = all_parts, target = target_of(draw.u, total), before = chosen_before;
     HeldRow<T, JOIN_ROUNDS> row = part_row<T, JOIN_ROUNDS>(a, r, chosen, JOIN_THREADS);
     if (m == INFINITY) row.only_infinite();
     u64 own[JOIN_ROUNDS];
-    const u64 here = CUT ? sum_values<JOIN_THREADS, true>(row, own, s.part64, kept.lowest(), kept) : sum_values<JOIN_THREADS, false>(row, own, s.part64, -INFINITY, kept);
+    const u64 here = sum_values<JOIN_THREADS, false>(row, own, s.part64, -INFINITY, kept);
     if (here == 0) {  // (a part whose weights are all below the point by themselves, if not by their sum: its largest)
         const float part_best = m == INFINITY ? 0.0f : in[chosen].best;
         int j = 0x7FFFFFFF;
