@@ -267,6 +267,15 @@ def sushi_subgraph_overlap(subnet_box, subgraph_box, bytes_per_weight=2):
 
 
 EINVAL = -1
+_DTYPE_NAMES = {}
+
+
+def _dtype_name(dtype):
+    """"float32" for torch.float32 (PyTorch itself is not imported here)."""
+    name = _DTYPE_NAMES.get(dtype)
+    if name is None:
+        name = _DTYPE_NAMES[dtype] = str(dtype)[len("torch."):]
+    return name
 
 
 def _refuse(what):
@@ -287,6 +296,8 @@ class Sushi:
         if rc != 0:
             raise SushiError(rc, (lib().sushi_last_error(None) or b"").decode())
         self.device = device
+        self._z, self._grad, self._sampling, self._teacher = CLogits(), CLogits(), CSampling(), CTeacher()
+        self._z_ref, self._sampling_ref, self._teacher_ref = C.byref(self._z), C.byref(self._sampling), C.byref(self._teacher)
         self.arch = None
         self.dtype = None
         self._cfg_cache = {}
@@ -395,32 +406,36 @@ class Sushi:
         return self._j.value
 
     # Operators on logits.  Device tensors in and out, as in sushi_infer: nothing is allocated, copied or converted here.
-    # What the C call cannot see of a tensor (its device, its type, its strides) is checked first.
+    # What the C call cannot see of a tensor (its device, its type, its strides) is checked first.  The structs are the
+    # context's own, filled again by every call.
     def _operand(self, t, what, dtype, shape):
         """Address of a contiguous tensor of that type (a name) and shape; None: NULL."""
         if t is None:
             return None
-        if str(t.dtype) != "torch." + dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        if _dtype_name(t.dtype) != dtype or t.shape != shape or not t.is_contiguous():
             _refuse("%s: a contiguous %s tensor of shape %s is needed" % (what, dtype, list(shape)))
-        if not t.is_cuda or t.device.index != self.device:
+        if t.get_device() != self.device:
             _refuse("%s: not on the context's device" % what)
         return t.data_ptr()
 
-    def _rows(self, t, what):
-        """(sushi_logits, type's name) of a tensor [rows, classes] whose rows are contiguous."""
-        name = str(t.dtype)[len("torch."):]
-        if name not in ("float32", "bfloat16") or t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+    def _rows(self, t, what, z):
+        """Fills z, a sushi_logits, with a tensor [rows, classes] whose rows are contiguous; returns (rows, type's name)."""
+        name = _dtype_name(t.dtype)
+        if (name != "float32" and name != "bfloat16") or t.dim() != 2:
             _refuse("%s: a float32 or bfloat16 tensor [rows, classes] with contiguous rows is needed" % what)
-        if not t.is_cuda or t.device.index != self.device:
+        (rows, classes), (stride, step) = t.shape, t.stride()
+        if classes < 1 or (classes > 1 and step != 1):
+            _refuse("%s: a float32 or bfloat16 tensor [rows, classes] with contiguous rows is needed" % what)
+        if t.get_device() != self.device:
             _refuse("%s: not on the context's device" % what)
-        rows, classes = t.shape
-        stride = t.stride(0) if rows > 1 else max(t.stride(0), classes)
-        return CLogits(t.data_ptr(), BF16 if name == "bfloat16" else FP32, rows, classes, stride), name
+        z.data, z.dtype, z.rows, z.classes = t.data_ptr(), BF16 if name == "bfloat16" else FP32, rows, classes
+        z.row_stride = stride if rows > 1 else max(stride, classes)
+        return rows, name
 
     def _workspace(self, t):
         if t is None:
             return None, 0
-        if not t.is_cuda or t.device.index != self.device or not t.is_contiguous():
+        if t.get_device() != self.device or not t.is_contiguous():
             _refuse("workspace: a contiguous tensor on the context's device is needed")
         return t.data_ptr(), t.numel() * t.element_size()
 
@@ -428,43 +443,50 @@ class Sushi:
                      workspace=None):
         """One class per row of logits [rows, classes], drawn with the random numbers uniform [rows] (float32).  classes: int32
         [rows] out; log_prob: float32 [rows] out or None; temperature, top_p, min_p (float32), top_k (int32): [rows] or None."""
-        z, _ = self._rows(logits, "logits")
-        n = (z.rows,)
-        s = CSampling(self._operand(temperature, "temperature", "float32", n), self._operand(top_k, "top_k", "int32", n),
-                      self._operand(top_p, "top_p", "float32", n), self._operand(min_p, "min_p", "float32", n))
-        _check(lib().sushi_sample(self._h, C.byref(z), C.byref(s), self._operand(uniform, "uniform", "float32", n),
-                                  self._operand(classes, "classes", "int32", n), self._operand(log_prob, "log_prob", "float32", n),
-                                  *self._workspace(workspace)), self._h)
+        n = (self._rows(logits, "logits", self._z)[0],)
+        s, f = self._sampling, self._operand
+        s.temperature, s.top_k = f(temperature, "temperature", "float32", n), f(top_k, "top_k", "int32", n)
+        s.top_p, s.min_p = f(top_p, "top_p", "float32", n), f(min_p, "min_p", "float32", n)
+        work, size = self._workspace(workspace)
+        rc = _lib.sushi_sample(self._h, self._z_ref, self._sampling_ref, f(uniform, "uniform", "float32", n),
+                               f(classes, "classes", "int32", n), f(log_prob, "log_prob", "float32", n), work, size)
+        if rc != 0:
+            _check(rc, self._h)
 
     def sushi_top_logits(self, logits, values, classes, rest=None, temperature=1.0, workspace=None):
         """The k leading logits of every row: values (float32) and classes (int32) [rows, k] out, rest (float32 [rows]) out or
         None: the probability outside them at the temperature."""
-        z, _ = self._rows(logits, "logits")
+        rows = self._rows(logits, "logits", self._z)[0]
         if values is None or values.dim() != 2:
             _refuse("values: a float32 tensor [rows, k] is needed")
-        shape = (z.rows, values.shape[1])
-        _check(lib().sushi_top_logits(self._h, C.byref(z), shape[1], temperature, self._operand(values, "values", "float32", shape),
-                                      self._operand(classes, "classes", "int32", shape),
-                                      self._operand(rest, "rest", "float32", (z.rows,)), *self._workspace(workspace)), self._h)
+        shape, f = (rows, values.shape[1]), self._operand
+        work, size = self._workspace(workspace)
+        rc = _lib.sushi_top_logits(self._h, self._z_ref, shape[1], temperature, f(values, "values", "float32", shape),
+                                   f(classes, "classes", "int32", shape), f(rest, "rest", "float32", (rows,)), work, size)
+        if rc != 0:
+            _check(rc, self._h)
 
     def sushi_distill(self, student, values, classes, loss, rest=None, temperature=1.0, weight=None, grad=None, workspace=None):
         """Loss of every row of student [rows, classes] against a teacher's list values (float32), classes (int32) [rows, k] with
         probability rest [rows] (None: 0) outside it: loss float32 [rows] out or None; grad (type and shape of student, rows
         contiguous; student itself is allowed) out or None: weight [rows] (None: 1) times the gradient."""
-        z, name = self._rows(student, "student")
+        rows, name = self._rows(student, "student", self._z)
         if values is None or values.dim() != 2:
             _refuse("values: a float32 tensor [rows, k] is needed")
-        shape, n = (z.rows, values.shape[1]), (z.rows,)
-        t = CTeacher(self._operand(values, "values", "float32", shape), self._operand(classes, "classes", "int32", shape),
-                     self._operand(rest, "rest", "float32", n), shape[1])
-        g = CLogits()
+        shape, n, t, f = (rows, values.shape[1]), (rows,), self._teacher, self._operand
+        t.values, t.classes = f(values, "values", "float32", shape), f(classes, "classes", "int32", shape)
+        t.rest, t.k = f(rest, "rest", "float32", n), shape[1]
+        at, stride = None, 0
         if grad is not None:
-            g, grad_name = self._rows(grad, "grad")
-            if grad_name != name or tuple(grad.shape) != tuple(student.shape):
+            g = self._grad
+            if self._rows(grad, "grad", g)[1] != name or grad.shape != student.shape:
                 _refuse("grad: the type and shape of student are needed")
-        _check(lib().sushi_distill(self._h, C.byref(z), C.byref(t), temperature, self._operand(weight, "weight", "float32", n),
-                                   self._operand(loss, "loss", "float32", n), g.data, g.row_stride, *self._workspace(workspace)),
-               self._h)
+            at, stride = g.data, g.row_stride
+        work, size = self._workspace(workspace)
+        rc = _lib.sushi_distill(self._h, self._z_ref, self._teacher_ref, temperature, f(weight, "weight", "float32", n),
+                                f(loss, "loss", "float32", n), at, stride, work, size)
+        if rc != 0:
+            _check(rc, self._h)
 
     def sushi_synchronize(self):
         _check(lib().sushi_synchronize(self._h), self._h)

@@ -133,18 +133,21 @@ class _Tensor:
     """What the binding looks at of a device tensor."""
 
     def __init__(self, shape, dtype="float32", stride=None, device=0, cuda=True, at=1 << 20):
-        self.shape, self.dtype, self.is_cuda, self.at = shape, "torch." + dtype, cuda, at
+        self.shape, self.dtype, self.at = shape, "torch." + dtype, at
         full = [1] * len(shape)
         for i in range(len(shape) - 2, -1, -1):
             full[i] = full[i + 1] * shape[i + 1]
         self.strides, self.contiguous = tuple(stride or full), not stride or list(stride) == full
-        self.device = type("Device", (), {"index": device})
+        self.index = device if cuda else -1
 
     def dim(self):
         return len(self.shape)
 
-    def stride(self, i):
-        return self.strides[i]
+    def stride(self):
+        return self.strides
+
+    def get_device(self):
+        return self.index
 
     def is_contiguous(self):
         return self.contiguous
