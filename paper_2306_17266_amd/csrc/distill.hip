@@ -16,7 +16,6 @@ namespace sushi {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int PART_PIECES = LOGITS_PART_PIECES;
 constexpr int LIST_BITS = 1 << 18;
 constexpr double LN2 = 6.931471805599453094e-01;
 
@@ -261,11 +260,9 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
 
 // ------------------------------------------------------------------ a row in parts
 
-__device__ __forceinline__ int first_index(int part, int per, int lead) { return part * PART_PIECES * per - lead; }
-
-template <typename T>
+template <typename T, int PIECES>
 __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, int row0, int parts, PartSums *out) {
-    constexpr int PER = 16 / sizeof(T), SPAN = PART_PIECES * PER;
+    constexpr int PER = 16 / sizeof(T), SPAN = PIECES * PER;
     __shared__ uint32_t bits[SPAN / 32];
     __shared__ int list[LOGITS_MAX_TOP];
     __shared__ int twice;
@@ -273,8 +270,8 @@ __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, in
     __shared__ double part_d[THREADS / 64];
     const long r = (long)row0 + blockIdx.x / parts;
     const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    HeldRow<T, PART_PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
-    const int origin = first_index(part, PER, row.lead);
+    HeldRow<T, PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PIECES, PIECES);
+    const int origin = part * SPAN - row.lead;
     mark_list<THREADS>(a, r, max(origin, 0), min(origin + SPAN, a.in.n), origin, SPAN - 1, bits, list, &twice);
     const float m = block_all<THREADS>(own_largest(row), part_f, larger);
     if (m == INFINITY) row.only_infinite();
@@ -312,16 +309,16 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     if (threadIdx.x == 0) out[blockIdx.x] = s;
 }
 
-template <typename T>
+template <typename T, int PIECES>
 __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a, int row0, int parts, const RowSums *in) {
-    constexpr int PER = 16 / sizeof(T), SPAN = PART_PIECES * PER, OWN = LOGITS_MAX_TOP / THREADS;
+    constexpr int PER = 16 / sizeof(T), SPAN = PIECES * PER, OWN = LOGITS_MAX_TOP / THREADS;
     __shared__ uint32_t bits[SPAN / 32];
     __shared__ int list[LOGITS_MAX_TOP];
     __shared__ int twice;
     const long r = (long)row0 + blockIdx.x / parts;
     const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Row<T> row(a.in, r, wave, THREADS / 64, lane, part * PART_PIECES, PART_PIECES);
-    const int origin = first_index(part, PER, row.lead), low = max(origin, 0), high = min(origin + SPAN, a.in.n);
+    Row<T> row(a.in, r, wave, THREADS / 64, lane, part * PIECES, PIECES);
+    const int origin = part * SPAN - row.lead, low = max(origin, 0), high = min(origin + SPAN, a.in.n);
     const RowSums s = in[blockIdx.x / parts];
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
     mark_list<THREADS>(a, r, low, high, origin, SPAN - 1, bits, list, &twice);
@@ -368,6 +365,23 @@ hipError_t launch_held(const DistillArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
+// most: rows of a launch.
+template <typename T, int PIECES>
+hipError_t launch_parts(const DistillArgs &a, int pieces, long most, char *ws, hipStream_t s) {
+    const int parts = logits_parts(pieces, PIECES);
+    RowSums *rows = reinterpret_cast<RowSums *>(ws);
+    PartSums *sums = reinterpret_cast<PartSums *>(ws + most * sizeof(RowSums));
+    for (long first = 0; first < a.in.rows; first += most) {
+        const int r = (int)first, n = (int)std::min<long>(a.in.rows - first, most);
+        distill_part_kernel<T, PIECES><<<n * parts, THREADS, 0, s>>>(a, r, parts, sums);
+        distill_row_kernel<T><<<n, THREADS, 0, s>>>(a, r, parts, sums, rows);
+        if (a.grad) distill_grad_kernel<T, PIECES><<<n * parts, THREADS, 0, s>>>(a, r, parts, rows);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <typename T>
 hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
     const int pieces = logits_pieces(a.in.n, a.in.bf16);
@@ -379,19 +393,8 @@ hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
         if (pieces <= 4096) return launch_held<T, 8, 512>(a, s);
         return launch_held<T, 8, 1024>(a, s);
     }
-    const int parts = logits_parts(a.in.n, a.in.bf16);
-    const long most = std::min<long>(rows_of_slice(a.in.n), a.in.rows);
-    RowSums *rows = reinterpret_cast<RowSums *>(ws);
-    PartSums *sums = reinterpret_cast<PartSums *>(ws + most * sizeof(RowSums));
-    for (long first = 0; first < a.in.rows; first += most) {
-        const int r = (int)first, n = (int)std::min<long>(a.in.rows - first, most);
-        distill_part_kernel<T><<<n * parts, THREADS, 0, s>>>(a, r, parts, sums);
-        distill_row_kernel<T><<<n, THREADS, 0, s>>>(a, r, parts, sums, rows);
-        if (a.grad) distill_grad_kernel<T><<<n * parts, THREADS, 0, s>>>(a, r, parts, rows);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    return small_parts(a.in) ? launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s)
+                             : launch_parts<T, LOGITS_PART_PIECES>(a, pieces, std::min<long>(rows_of_slice(a.in.n), a.in.rows), ws, s);
 }
 
 }  // namespace
@@ -400,9 +403,11 @@ size_t distill_part_bytes() { return sizeof(PartSums); }
 size_t distill_row_bytes() { return sizeof(RowSums); }
 
 size_t logits_workspace_bytes(int rows, int n) {
-    const size_t slice = std::min<long>(rows_of_slice(n), rows), parts = slice * logits_parts(n, false);
-    return std::max({parts * distill_part_bytes() + slice * distill_row_bytes(), parts * sample_part_bytes() + slice * sample_row_bytes(),
-                     parts * top_logits_part_bytes()});
+    const int pieces = logits_pieces(n, false);
+    const size_t slice = std::min<long>(rows_of_slice(n), rows), parts = slice * logits_parts(pieces, LOGITS_PART_PIECES);
+    const size_t few = std::min(rows, LOGITS_MOST_SMALL_PARTS), small = std::min<size_t>(few * logits_parts(pieces, LOGITS_SMALL_PART_PIECES), LOGITS_MOST_SMALL_PARTS);
+    return std::max({std::max(parts, small) * distill_part_bytes() + std::max(slice, few) * distill_row_bytes(),
+                     std::max(parts, small) * sample_part_bytes() + std::max(slice, few) * sample_row_bytes(), parts * top_logits_part_bytes()});
 }
 
 hipError_t launch_distill(const DistillArgs &a, void *ws, hipStream_t s) {

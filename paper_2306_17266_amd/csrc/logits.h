@@ -55,20 +55,27 @@ struct DistillArgs {
 };
 
 // Rows are read in pieces of 16 bytes.  A row that fits the registers of a workgroup is one workgroup's; longer rows, and long ones
-// where there are few, are read in parts of LOGITS_PART_PIECES, a workgroup each, whose results a workgroup per row joins.
+// where there are few, are read in parts, a workgroup each, whose results a workgroup per row joins.
 constexpr int LOGITS_PART_PIECES = 2048;
+constexpr int LOGITS_SMALL_PART_PIECES = 512;  // where few rows would leave compute units without a part
+constexpr int LOGITS_MOST_SMALL_PARTS = 1024;  // of all rows
+constexpr int LOGITS_MOST_PARTS = LOGITS_MAX_CLASSES / (4 * LOGITS_PART_PIECES) + 1;  // of a row
 inline int logits_pieces(int n, bool bf16) {  // (a row may start inside its first piece)
     const int per = bf16 ? 8 : 4;
     return (n + 2 * per - 2) / per;
 }
-inline int logits_parts(int n, bool bf16) { return (logits_pieces(n, bf16) + LOGITS_PART_PIECES - 1) / LOGITS_PART_PIECES; }
+inline int logits_parts(int pieces, int part_pieces) { return (pieces + part_pieces - 1) / part_pieces; }
 inline bool held_rows(const LogitRows &in) {
     const int pieces = logits_pieces(in.n, in.bf16);
     return pieces <= 1024 || (pieces <= 8192 && in.rows >= 192);
 }
+inline bool small_parts(const LogitRows &in) {
+    const int parts = logits_parts(logits_pieces(in.n, in.bf16), LOGITS_SMALL_PART_PIECES);
+    return parts <= LOGITS_MOST_PARTS && (long)in.rows * parts <= LOGITS_MOST_SMALL_PARTS;
+}
 // Rows that go out in one launch in parts (for both types alike): what a call needs of the workspace stays bounded.
 inline long rows_of_slice(int n) {
-    const long rows = 4096 / logits_parts(n, false);
+    const long rows = 4096 / logits_parts(logits_pieces(n, false), LOGITS_PART_PIECES);
     return rows > 1 ? rows : 1;
 }
 // Of the workspace: bytes that an operator needs for each part, and for each row.

@@ -245,10 +245,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
 
 // ------------------------------------------------------------------ a row in parts
 
-constexpr int PART_THREADS = 256, PART_ROUNDS = LOGITS_PART_PIECES / PART_THREADS, JOIN_THREADS = 1024;
-constexpr int JOIN_ROUNDS = LOGITS_PART_PIECES / JOIN_THREADS;
+constexpr int PART_THREADS = 256, JOIN_THREADS = 1024;
 constexpr int LIST = 4096;  // members of the interval in which a row is cut that are kept for its last step
-constexpr int MOST_PARTS = LOGITS_MAX_CLASSES / (4 * LOGITS_PART_PIECES) + 1;
+constexpr int MOST_PARTS = LOGITS_MOST_PARTS;
 
 // What a part has of its row: its maximum and how often; the histogram over a grid that all parts of the row share (place 0 is the
 // logit 0), from the maximum's interval on, without what equals the maximum; or, without filters, the sum of its weights.
@@ -271,18 +270,25 @@ struct SampleRow {
     u64 entry[LIST];
 };
 
-template <typename T, int N>
-__device__ __forceinline__ HeldRow<T, N> part_row(const SampleArgs &a, long r, int part, int threads) {
-    return HeldRow<T, N>(a.in, r, threadIdx.x >> 6, threads / 64, threadIdx.x & 63, part * LOGITS_PART_PIECES, LOGITS_PART_PIECES);
+template <typename T, int PIECES, int THREADS>
+using PartRow = HeldRow<T, (PIECES + THREADS - 1) / THREADS>;
+template <typename T, int PIECES, int THREADS>
+__device__ __forceinline__ PartRow<T, PIECES, THREADS> part_row(const SampleArgs &a, long r, int part) {
+    // (a workgroup with more threads than pieces: waves without any)
+    constexpr int WAVES = PIECES < THREADS ? PIECES / 64 : THREADS / 64;
+    const int wave = threadIdx.x >> 6;
+    PartRow<T, PIECES, THREADS> row(a.in, r, wave < WAVES ? wave : 0, WAVES, threadIdx.x & 63, part * PIECES, PIECES);
+    if (wave >= WAVES) row.rounds = 0;
+    return row;
 }
 
 // First launch.  CUT: histograms; else sums.
-template <typename T, bool CUT>
+template <typename T, int PIECES, bool CUT>
 __global__ __launch_bounds__(PART_THREADS) void sample_part_kernel(SampleArgs a, int row0, int parts, SamplePart *out) {
     __shared__ SearchLds s;
     __shared__ double part_d[PART_THREADS / 64];
     const long r = (long)row0 + blockIdx.x / parts;
-    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
+    PartRow<T, PIECES, PART_THREADS> row = part_row<T, PIECES, PART_THREADS>(a, r, blockIdx.x % parts);
     const Draw draw(a, r);
     SamplePart &mine = out[blockIdx.x];
     const float m = largest<PART_THREADS>(row, s.part_f);
@@ -300,7 +306,7 @@ __global__ __launch_bounds__(PART_THREADS) void sample_part_kernel(SampleArgs a,
         return;
     }
     const Grid grid(best, inv_t, 0.0);
-    const Packed packed(LOGITS_PART_PIECES * HeldRow<T, PART_ROUNDS>::PER);
+    const Packed packed(LOGITS_PART_PIECES * (16 / (int)sizeof(T)));
     build_histogram<PART_THREADS>(row, grid, packed, s);
     u64 both = 0;
     row.each([&](float z, int) { both += (u64)(z == best) + ((u64)(z > -INFINITY) << 32); });
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a,
     __syncthreads();
     uint32_t count[1] = {0}, equal = 0, ordered = 0;
     u64 lacking[1] = {0};
-    constexpr int BATCH = 8;  // (their loads are on the way together)
+    constexpr int BATCH = 16;  // (their loads are on the way together)
     for (int first = 0; first < parts; first += BATCH) {
         u64 v[BATCH];
 #pragma unroll
@@ -382,7 +388,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a,
 }
 
 // Third launch: each part lists its members of that interval, and sums the weights above it (from its histogram).
-template <typename T>
+template <typename T, int PIECES>
 __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs a, int row0, int parts, SamplePart *part_out, SampleRow *rows) {
     __shared__ double part_d[PART_THREADS / 64];
     __shared__ int n, at;
@@ -390,7 +396,7 @@ __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs 
     const long r = (long)row0 + blockIdx.x / parts;
     SampleRow &state = rows[blockIdx.x / parts];
     SamplePart &mine = part_out[blockIdx.x];
-    HeldRow<T, PART_ROUNDS> row = part_row<T, PART_ROUNDS>(a, r, blockIdx.x % parts, PART_THREADS);
+    PartRow<T, PIECES, PART_THREADS> row = part_row<T, PIECES, PART_THREADS>(a, r, blockIdx.x % parts);
     u64 v[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i) v[i] = mine.weight[i * PART_THREADS + threadIdx.x];
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs 
     const float best = m == INFINITY ? 0.0f : m, own_best = part_best == INFINITY ? 0.0f : part_best;
     const double inv_t = 1.0 / (double)draw.temperature;
     const Grid grid(best, inv_t, 0.0);
-    const Packed packed(LOGITS_PART_PIECES * HeldRow<T, PART_ROUNDS>::PER);
+    const Packed packed(LOGITS_PART_PIECES * (16 / (int)sizeof(T)));
     const int fraction = fraction_bits(a.in.n);
     if (threadIdx.x == 0) n = 0;
     // weights of the part's intervals before the row's `start`
@@ -460,7 +466,7 @@ struct Listed {
 };
 
 // Last launch, a workgroup per row: the cut, the part in which the running sum passes the target, and the class there.
-template <typename T, bool CUT>
+template <typename T, int PIECES, bool CUT>
 __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs a, int row0, int parts, const SamplePart *in, const SampleRow *rows) {
     __shared__ SearchLds s;
     __shared__ u64 sums[MOST_PARTS];
@@ -498,7 +504,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
             // the kept members, to the sums of their parts
             auto add = [&](float z, int j) {
                 const uint32_t k = order_key(z);
-                if (k >= low && k <= high) atomicAdd(&sums[(j + whole.lead) / (LOGITS_PART_PIECES * PER)], kept(z, j));
+                if (k >= low && k <= high) atomicAdd(&sums[(j + whole.lead) / (PIECES * PER)], kept(z, j));
             };
             if (listed.n <= LIST)
                 listed.each_from(key_value(low), add);
@@ -539,9 +545,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
     }
     __syncthreads();
     const u64 total = all_parts, target = target_of(draw.u, total), before = chosen_before;
-    HeldRow<T, JOIN_ROUNDS> row = part_row<T, JOIN_ROUNDS>(a, r, chosen, JOIN_THREADS);
+    PartRow<T, PIECES, JOIN_THREADS> row = part_row<T, PIECES, JOIN_THREADS>(a, r, chosen);
     if (m == INFINITY) row.only_infinite();
-    u64 own[JOIN_ROUNDS];
+    u64 own[(PIECES + JOIN_THREADS - 1) / JOIN_THREADS];
     const u64 here = sum_values<JOIN_THREADS, false>(row, own, s.part64, -INFINITY, kept);
     if (here == 0) {  // (a part whose weights are all below the point by themselves, if not by their sum: its largest)
         const float part_best = m == INFINITY ? 0.0f : in[chosen].best;
@@ -556,27 +562,34 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
                                [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
 }
 
-template <typename T>
-hipError_t launch(const SampleArgs &a, char *ws, hipStream_t s) {
-    if (held_rows(a.in))
-        return by_size(logits_pieces(a.in.n, a.in.bf16), [&](auto N, auto THREADS) {
-            return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { sample_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
-        });
-    const int parts = logits_parts(a.in.n, a.in.bf16);
-    const long most = rows_of_slice(a.in.n) < a.in.rows ? rows_of_slice(a.in.n) : a.in.rows;
+// most: rows of a launch.
+template <typename T, int PIECES>
+hipError_t launch_parts(const SampleArgs &a, int pieces, long most, char *ws, hipStream_t s) {
+    const int parts = logits_parts(pieces, PIECES);
     SampleRow *rows = reinterpret_cast<SampleRow *>(ws);
     SamplePart *sums = reinterpret_cast<SamplePart *>(ws + most * sizeof(SampleRow));
     return by_slices(a.in.rows, most, [&](int r, int n) {
         if (a.top_k || a.top_p || a.min_p) {
-            sample_part_kernel<T, true><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
+            sample_part_kernel<T, PIECES, true><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
             sample_join_kernel<<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
-            sample_gather_kernel<T><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums, rows);
-            sample_finish_kernel<T, true><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
+            sample_gather_kernel<T, PIECES><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums, rows);
+            sample_finish_kernel<T, PIECES, true><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
         } else {
-            sample_part_kernel<T, false><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
-            sample_finish_kernel<T, false><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
+            sample_part_kernel<T, PIECES, false><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
+            sample_finish_kernel<T, PIECES, false><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
         }
     });
+}
+
+template <typename T>
+hipError_t launch(const SampleArgs &a, char *ws, hipStream_t s) {
+    const int pieces = logits_pieces(a.in.n, a.in.bf16);
+    if (held_rows(a.in))
+        return by_size(pieces, [&](auto N, auto THREADS) {
+            return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { sample_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
+        });
+    if (small_parts(a.in)) return launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s);
+    return launch_parts<T, LOGITS_PART_PIECES>(a, pieces, rows_of_slice(a.in.n) < a.in.rows ? rows_of_slice(a.in.n) : a.in.rows, ws, s);
 }
 
 }  // namespace

@@ -343,7 +343,7 @@ hipError_t launch(const TopArgs &a, TopPart *ws, hipStream_t s) {
         return by_size(logits_pieces(a.in.n, a.in.bf16), [&](auto N, auto THREADS) {
             return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { top_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
         });
-    const int parts = logits_parts(a.in.n, a.in.bf16);
+    const int parts = logits_parts(logits_pieces(a.in.n, a.in.bf16), LOGITS_PART_PIECES);
     return by_slices(a.in.rows, rows_of_slice(a.in.n), [&](int r, int n) {
         top_part_kernel<T><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, ws);
         top_join_kernel<T><<<n, JOIN_THREADS, 0, s>>>(a, r, parts, ws);
