@@ -75,7 +75,7 @@ inline bool small_parts(const LogitRows &in) {
 }
 // Rows that go out in one launch in parts (for both types alike): what a call needs of the workspace stays bounded.
 inline long rows_of_slice(int n) {
-    const long rows = 4096 / logits_parts(logits_pieces(n, false), LOGITS_PART_PIECES);
+    const long rows = 8192 / logits_parts(logits_pieces(n, false), LOGITS_PART_PIECES);
     return rows > 1 ? rows : 1;
 }
 // Of the workspace: bytes that an operator needs for each part, and for each row.

@@ -254,6 +254,7 @@ constexpr int MOST_PARTS = LOGITS_MOST_PARTS;
 struct SamplePart {
     float best;
     uint32_t equal, ordered;  // logits that equal the maximum, that are above -inf
+    int used;                 // intervals up to the last that is not empty; what is behind is not written
     double top, sum;
     u64 kept;  // sum of the weights that are kept whatever the list says
     u64 weight[BINS];
@@ -308,75 +309,87 @@ __global__ __launch_bounds__(PART_THREADS) void sample_part_kernel(SampleArgs a,
     const Grid grid(best, inv_t, 0.0);
     const Packed packed(LOGITS_PART_PIECES * (16 / (int)sizeof(T)));
     build_histogram<PART_THREADS>(row, grid, packed, s);
-    u64 both = 0;
-    row.each([&](float z, int) { both += (u64)(z == best) + ((u64)(z > -INFINITY) << 32); });
-    both = block_sum<PART_THREADS>(both, s.part64);
-    if (threadIdx.x == 0) {
-        const double t = grid.place(best);
-        s.weight[0] -= (both & 0xFFFFFFFFu) * packed.one(t - floor(t));
-        mine.equal = (uint32_t)both, mine.ordered = (uint32_t)(both >> 32), mine.top = grid.top;
+    uint32_t equal = 0;
+    row.each([&](float z, int) { equal += __popcll(__ballot(z == best)); });  // (of the wave)
+    uint32_t ordered = 0;
+    int used = 0;
+    for (int b = threadIdx.x; b < BINS; b += PART_THREADS) {
+        const uint32_t n = packed.count(s.weight[b]);
+        ordered += n, used = n ? b + 1 : used;
     }
+    ordered = wave_sum(ordered), used = wave_all(used, [](int p, int q) { return p > q ? p : q; });
+    if ((threadIdx.x & 63) == 0) s.part32[threadIdx.x >> 6] = equal, s.part32[4 + (threadIdx.x >> 6)] = ordered, s.count[threadIdx.x >> 6] = used;
     __syncthreads();
-    for (int b = threadIdx.x; b < BINS; b += PART_THREADS) mine.weight[b] = s.weight[b];
+    equal = s.part32[0] + s.part32[1] + s.part32[2] + s.part32[3], ordered = s.part32[4] + s.part32[5] + s.part32[6] + s.part32[7];
+    used = max(max(s.count[0], s.count[1]), max(s.count[2], s.count[3]));
+    const double t = grid.place(best);
+    for (int b = threadIdx.x; b < used; b += PART_THREADS) mine.weight[b] = s.weight[b] - (b == 0 ? equal * packed.one(t - floor(t)) : 0);
+    if (threadIdx.x == 0) mine.equal = equal, mine.ordered = ordered, mine.used = used, mine.top = grid.top;
 }
 
 // Second launch, a workgroup per row: the joined histogram, and where the row is cut.
 __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a, int row0, int parts, const SamplePart *in, SampleRow *out) {
     __shared__ SearchLds s;
-    __shared__ double top[MOST_PARTS];
-    __shared__ float maxima[MOST_PARTS];
-    __shared__ uint32_t n_equal[MOST_PARTS], n_ordered[MOST_PARTS];
+    __shared__ int down[MOST_PARTS], used[MOST_PARTS];
+    __shared__ uint32_t sums[2];
     static_assert(BINS == JOIN_THREADS, "a thread has one interval");
     const long r = (long)row0 + blockIdx.x;
     in += (long)blockIdx.x * parts;
     SampleRow &row = out[blockIdx.x];
     const Draw draw(a, r);
-    float m = -INFINITY;
+    float part_best = -INFINITY;
+    double top = 0.0;
+    uint32_t part_equal = 0, part_ordered = 0;
+    int part_used = 0;
     if ((int)threadIdx.x < parts) {
         const SamplePart &p = in[threadIdx.x];
-        m = maxima[threadIdx.x] = p.best, top[threadIdx.x] = p.top, n_equal[threadIdx.x] = p.equal, n_ordered[threadIdx.x] = p.ordered;
+        part_best = p.best, top = p.top, part_equal = p.equal, part_ordered = p.ordered, part_used = p.used;
     }
     s.count[threadIdx.x] = 0, s.weight[threadIdx.x] = 0;
-    m = block_all<JOIN_THREADS>(m, s.part_f, [](float p, float q) { return fmaxf(p, q); });
+    if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+    const float m = block_all<JOIN_THREADS>(part_best, s.part_f, [](float p, float q) { return fmaxf(p, q); });
     if (threadIdx.x == 0) row.best = m, row.n = 0, row.start = BINS, s.before = 0, s.weight_before = 0;
     if (m == -INFINITY || !draw.cuts(a.in.n)) return;
     const float best = m == INFINITY ? 0.0f : m;
     const int fraction = fraction_bits(a.in.n);
     const Grid grid(best, 1.0 / (double)draw.temperature, 0.0);
     const Packed packed(LOGITS_PART_PIECES * (a.in.bf16 ? 8 : 4));
+    if ((int)threadIdx.x < parts) {
+        const bool counts = part_best > -INFINITY && (m < INFINITY || part_best == INFINITY);
+        // the part's intervals lie that much further down
+        const int d = counts ? (int)fmin(top - grid.top, (double)BINS) : BINS;
+        down[threadIdx.x] = d, used[threadIdx.x] = part_used;
+        if (counts) {
+            atomicAdd(&sums[0], part_ordered);
+            if (part_best == m) {
+                atomicAdd(&sums[1], part_equal);
+            } else if (d < BINS - 1) {  // what equals the part's maximum, at its own place
+                const double t = grid.place(part_best);
+                atomicAdd(&s.count[d], part_equal);
+                atomicAdd(&s.weight[d], part_equal * packed.lack(packed.one(t - floor(t))));
+            }
+        }
+    }
     __syncthreads();
-    uint32_t count[1] = {0}, equal = 0, ordered = 0;
+    uint32_t count[1] = {0};
     u64 lacking[1] = {0};
     constexpr int BATCH = 16;  // (their loads are on the way together)
     for (int first = 0; first < parts; first += BATCH) {
         u64 v[BATCH];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) v[i] = in[min(first + i, parts - 1)].weight[threadIdx.x];
-#pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int p = first + i;
-            if (p >= parts || maxima[p] == -INFINITY || (m == INFINITY && maxima[p] < INFINITY)) continue;
-            ordered += n_ordered[p];
-            if (maxima[p] == m) equal += n_equal[p];
-            // the part's intervals lie `down` further down
-            const int down = (int)fmin(top[p] - grid.top, (double)BINS), to = (int)threadIdx.x + down;
-            if (down == 0 && threadIdx.x < BINS - 1) {
-                count[0] += packed.count(v[i]), lacking[0] += packed.lack(v[i]);
-            } else if (to < BINS - 1 && v[i]) {
-                atomicAdd(&s.count[to], packed.count(v[i]));
-                atomicAdd(&s.weight[to], packed.lack(v[i]));
-            }
-            if (threadIdx.x == 0 && maxima[p] < m && down < BINS - 1) {  // what equals the part's maximum, at its own place
-                const double t = grid.place(maxima[p]);
-                atomicAdd(&s.count[down], n_equal[p]);
-                atomicAdd(&s.weight[down], n_equal[p] * packed.lack(packed.one(t - floor(t))));
-            }
+            const int p = first + i, b = p < parts ? (int)threadIdx.x - down[p] : -1;
+            v[i] = 0;
+            if (b >= 0 && b < used[min(p, parts - 1)]) v[i] = in[p].weight[b];
         }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) count[0] += packed.count(v[i]), lacking[0] += packed.lack(v[i]);
     }
-    __syncthreads();
-    count[0] += s.count[threadIdx.x], lacking[0] += s.weight[threadIdx.x];
+    const uint32_t ordered = sums[0], equal = sums[1];
+    count[0] = threadIdx.x < BINS - 1 ? count[0] + s.count[threadIdx.x] : 0;
+    lacking[0] += s.weight[threadIdx.x];
     // what falls off the end, in the last interval
-    const uint32_t placed = block_sum<JOIN_THREADS>(threadIdx.x < BINS - 1 ? count[0] : 0u, s.part32);
+    const uint32_t placed = block_sum<JOIN_THREADS>(count[0], s.part32);
     if (threadIdx.x == BINS - 1) count[0] = ordered - placed - equal;
     __syncthreads();
     Limit limit{(uint32_t)draw.k, INFINITY};
@@ -397,9 +410,13 @@ __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs 
     SampleRow &state = rows[blockIdx.x / parts];
     SamplePart &mine = part_out[blockIdx.x];
     PartRow<T, PIECES, PART_THREADS> row = part_row<T, PIECES, PART_THREADS>(a, r, blockIdx.x % parts);
+    const int used = mine.used;
     u64 v[OWN];
 #pragma unroll
-    for (int i = 0; i < OWN; ++i) v[i] = mine.weight[i * PART_THREADS + threadIdx.x];
+    for (int i = 0; i < OWN; ++i) {
+        v[i] = 0;
+        if (i * PART_THREADS + (int)threadIdx.x < used) v[i] = mine.weight[i * PART_THREADS + threadIdx.x];
+    }
     const float m = state.best, part_best = mine.best;
     const uint32_t low = state.low, high = state.high;
     const int start = state.start;
@@ -453,14 +470,23 @@ __global__ __launch_bounds__(PART_THREADS) void sample_gather_kernel(SampleArgs 
         });
 }
 
-// A row's list.
+// A row's list, in registers.
 struct Listed {
-    const u64 *entry;
-    int n;
+    static constexpr int OWN = LIST / JOIN_THREADS;
+    u64 entry[OWN];
+    __device__ __forceinline__ void load(const u64 *from) {  // (whether or not there is something: the loads need not wait for the number)
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) entry[i] = from[i * JOIN_THREADS + threadIdx.x];
+    }
+    __device__ __forceinline__ void limit_to(int n) {
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) entry[i] = i * JOIN_THREADS + (int)threadIdx.x < n ? entry[i] : 0;
+    }
     template <typename F>
     __device__ __forceinline__ void each_from(float z_low, F f) const {
         const uint32_t low = order_key(z_low);
-        for (int i = threadIdx.x; i < n; i += JOIN_THREADS)
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
             if ((uint32_t)(entry[i] >> 32) >= low) f(key_value((uint32_t)(entry[i] >> 32)), (int)(uint32_t)entry[i]);
     }
 };
@@ -476,10 +502,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
     const long r = (long)row0 + blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     in += (long)blockIdx.x * parts;
+    Listed listed;
+    if (CUT) listed.load(rows[blockIdx.x].entry);
     const Draw draw(a, r);
     Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
     float m = -INFINITY;
-    if ((int)threadIdx.x < parts) m = in[threadIdx.x].best;
+    u64 part_kept = 0;
+    if ((int)threadIdx.x < parts) {
+        m = in[threadIdx.x].best;
+        if (CUT) part_kept = in[threadIdx.x].kept;
+    }
     const float mine = m;
     m = block_all<JOIN_THREADS>(m, s.part_f, [](float p, float q) { return fmaxf(p, q); });
     if (m == -INFINITY) {
@@ -494,19 +526,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
         const uint32_t low = state.low, high = state.high;
         const int start = state.start;
         if (threadIdx.x == 0) s.before = state.before, s.weight_before = state.weight_before, s.inside = state.inside;
-        if ((int)threadIdx.x < parts) sums[threadIdx.x] = in[threadIdx.x].kept;
+        if ((int)threadIdx.x < parts) sums[threadIdx.x] = part_kept;
         __syncthreads();
         if (start < BINS) {
             const Limit limit{(uint32_t)draw.k, state.limit};
-            const Listed listed{state.entry, state.n};
-            kept.cut = listed.n <= LIST ? cut_among<JOIN_THREADS, true>(listed, whole, kept.weight, s, limit, low, high, kept.fraction)
+            const bool all = state.n <= LIST;
+            listed.limit_to(state.n);
+            kept.cut = all ? cut_among<JOIN_THREADS, true>(listed, whole, kept.weight, s, limit, low, high, kept.fraction)
                                         : cut_among<JOIN_THREADS, true>(whole, whole, kept.weight, s, limit, low, high, kept.fraction);
             // the kept members, to the sums of their parts
             auto add = [&](float z, int j) {
                 const uint32_t k = order_key(z);
                 if (k >= low && k <= high) atomicAdd(&sums[(j + whole.lead) / (PIECES * PER)], kept(z, j));
             };
-            if (listed.n <= LIST)
+            if (all)
                 listed.each_from(key_value(low), add);
             else
                 whole.each_from(key_value(low), add);
