@@ -96,6 +96,16 @@ struct Terms : Weight {
     __device__ __forceinline__ double log2_of(float z) const { return Weight::log2_of(infinite ? as_infinite(z) : z); }
 };
 
+// What belongs to a row besides its logits and its list; loaded before it is needed.
+struct RowInputs {
+    float rest, weight;
+    __device__ __forceinline__ RowInputs(const DistillArgs &a, long r) {
+        const float *any = reinterpret_cast<const float *>(a.classes);  // (without a branch for each)
+        rest = (a.rest ? a.rest : any)[r], weight = (a.weight ? a.weight : any)[r];
+        rest = a.rest ? rest : 0.0f, weight = a.weight ? weight : 1.0f;
+    }
+};
+
 // This thread's entries of a row's list.
 template <int OWN>
 struct Entries {
@@ -130,7 +140,7 @@ __device__ __forceinline__ void maxima(float &m, float &tm, const Entries<OWN> &
 // The row's loss (written) and what its gradient needs, from the maxima and each thread's part of R.  Only the waves that have
 // entries compute with them.
 template <int THREADS, int OWN>
-__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, float m, float tm, double rest, const Entries<OWN> &own, double (*part)[THREADS / 64]) {
+__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, const RowInputs &row, float m, float tm, double rest, const Entries<OWN> &own, double (*part)[THREADS / 64]) {
     const int wave = threadIdx.x >> 6;
     const bool entries = wave * 64 < a.k;
     const double inv_t = 1.0 / (double)a.temperature;
@@ -147,7 +157,7 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, floa
     __syncthreads();
     rest = sum_across<THREADS / 64>(part[0]), sum = rest + sum_across<THREADS / 64>(part[1]), list_sum = sum_across<THREADS / 64>(part[2]);
     const bool nan = m != m || tm != tm;
-    double mass = a.rest ? (double)a.rest[r] : 0.0;  // outside the list
+    double mass = row.rest;  // outside the list
     mass = mass < 0.0 ? 0.0 : mass > 1.0 ? 1.0 : mass;
     const bool empty = !nan && (m == -INFINITY || tm == -INFINITY);
     if (a.loss) {
@@ -172,7 +182,7 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, floa
         }
         if (threadIdx.x == 0) a.loss[r] = empty ? 0.0f : nan ? NAN : (float)loss;
     }
-    const float w = empty ? 0.0f : a.weight ? a.weight[r] : 1.0f;
+    const float w = empty ? 0.0f : row.weight;
     const double inv_sum = 1.0 / sum, share = mass == 0.0 ? inv_sum : rest > 0.0 ? inv_sum - mass / rest : 0.0;
     return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan ? NAN : w * inv_t * share, m, tm, (float)(w * inv_t), 0.0f};
 }
@@ -216,6 +226,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
     __shared__ double part_d[4][THREADS / 64];
     const long r = (long)row0 + blockIdx.x;
     HeldRow<T, N> row(a.in, r, threadIdx.x >> 6, THREADS / 64, threadIdx.x & 63);
+    const RowInputs inputs(a, r);
     mark_list<THREADS>(a, r, 0, a.in.n, -row.lead, SPAN - 1, bits, list, &twice);
     const Entries<OWN> own = read_entries<T, THREADS, OWN>(a, r, list, twice);
     float m = own_largest(row), tm;
@@ -226,7 +237,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
     const Weight weight(m == INFINITY ? 0.0f : m, inv_t);
     double rest = 0.0;
     row.each([&](float z, int) { rest += exp2_64<6>(weight.log2_of(z)); });
-    const RowSums s = finish_row<THREADS>(a, r, m, tm, rest, own, part_d);
+    const RowSums s = finish_row<THREADS>(a, r, inputs, m, tm, rest, own, part_d);
     if (!a.grad) return;
     // (the gradient may take the logits' place: every thread has passed a barrier since its logits were read)
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
@@ -293,6 +304,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     constexpr int OWN = LOGITS_MAX_TOP / THREADS;
     const long r = (long)row0 + blockIdx.x;
     const int n = a.in.n;
+    const RowInputs inputs(a, r);
     uint32_t mask = 31;
     while ((int)mask + 1 < n && mask + 1 < LIST_BITS) mask = mask * 2 + 1;
     mark_list<THREADS>(a, r, 0, n, 0, mask, bits, list, &twice);
@@ -305,7 +317,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     double rest = 0.0;
     for (int p = threadIdx.x; p < parts; p += THREADS)
         if (in[p].rest != 0.0) rest += in[p].rest * exp2_64<11>(student.log2_of(in[p].best));
-    const RowSums s = finish_row<THREADS>(a, r, m, tm, rest, own, part_d);
+    const RowSums s = finish_row<THREADS>(a, r, inputs, m, tm, rest, own, part_d);
     if (threadIdx.x == 0) out[blockIdx.x] = s;
 }
 
@@ -393,7 +405,7 @@ hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
         if (pieces <= 4096) return launch_held<T, 8, 512>(a, s);
         return launch_held<T, 8, 1024>(a, s);
     }
-    return small_parts(a.in) ? launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s)
+    return small_parts(a.in, LOGITS_MOST_PARTS) ? launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s)
                              : launch_parts<T, LOGITS_PART_PIECES>(a, pieces, std::min<long>(rows_of_slice(a.in.n), a.in.rows), ws, s);
 }
 
@@ -406,7 +418,9 @@ size_t logits_workspace_bytes(int rows, int n) {
     const int pieces = logits_pieces(n, false);
     const size_t slice = std::min<long>(rows_of_slice(n), rows), parts = slice * logits_parts(pieces, LOGITS_PART_PIECES);
     const size_t few = std::min(rows, LOGITS_MOST_SMALL_PARTS), small = std::min<size_t>(few * logits_parts(pieces, LOGITS_SMALL_PART_PIECES), LOGITS_MOST_SMALL_PARTS);
-    return std::max({std::max(parts, small) * distill_part_bytes() + std::max(slice, few) * distill_row_bytes(),
+    const size_t distill = std::max(parts, small) * distill_part_bytes() + std::max(slice, few) * distill_row_bytes();
+    if (n <= LOGITS_HELD_PLAIN_FEW) return distill;  // (the others hold these rows, of either type)
+    return std::max({distill,
                      std::max(parts, small) * sample_part_bytes() + std::max(slice, few) * sample_row_bytes(), parts * top_logits_part_bytes()});
 }
 

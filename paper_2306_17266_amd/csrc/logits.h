@@ -54,8 +54,8 @@ struct DistillArgs {
     long grad_stride;  // elements from row to row
 };
 
-// Rows are read in pieces of 16 bytes.  A row that fits the registers of a workgroup is one workgroup's; longer rows, and long ones
-// where there are few, are read in parts, a workgroup each, whose results a workgroup per row joins.
+// Rows are read in pieces of 16 bytes.  A row that fits the registers of a workgroup is one workgroup's, who reads it once; longer
+// rows, and long ones where there are few, are read in parts, a workgroup each, whose results a workgroup per row joins.
 constexpr int LOGITS_PART_PIECES = 2048;
 constexpr int LOGITS_SMALL_PART_PIECES = 512;  // where few rows would leave compute units without a part
 constexpr int LOGITS_MOST_SMALL_PARTS = 1024;  // of all rows
@@ -65,13 +65,34 @@ inline int logits_pieces(int n, bool bf16) {  // (a row may start inside its fir
     return (n + 2 * per - 2) / per;
 }
 inline int logits_parts(int pieces, int part_pieces) { return (pieces + part_pieces - 1) / part_pieces; }
+
+// Whether rows are held.  Measured, in parts against held, in us:
+//                                                   rows = 16                    rows = 256
+//   float32 x  16000: sample, its plain form      25.1 - 17.8, 10.0 - 11.1     34.4 - 18.1, 14.2 - 11.4
+//                     top, loss, loss + gradient  18.7 - 11.5, 10.2 - 7.5, 14.3 - 8.6
+//   float32 x  32000: sample, its plain form      25.4 - 20.7,  9.8 - 16.5     42.7 - 23.5, 19.3 - 18.0
+//                     top, loss, loss + gradient  19.1 - 14.1, 10.1 - 9.8, 14.0 - 11.9
+//   bf16    x  32000: sample, its plain form      26.7 - 27.9, 10.0 - 18.1     41.7 - 27.0, 20.1 - 18.5
+//   bf16    x  64000: sample, its plain form      28.0 - 31.5, 10.4 - 27.9     55.2 - 33.1, 27.7 - 29.1
+//                     top, loss, loss + gradient  21.4 - 21.1, 10.1 - 14.6, 13.9 - 18.4 (37.9 - 23.8, 20.8 - 15.9, 32.6 - 23.5)
+// The plain form of sampling (no top_k, top_p, min_p) computes an exponential for each logit and little else, and gains by more
+// compute units sooner.
+constexpr int LOGITS_HELD_PIECES = 8192, LOGITS_HELD_PLAIN_PIECES = 4096;
+constexpr int LOGITS_HELD_FEW = 32000, LOGITS_HELD_PLAIN_FEW = 16000, LOGITS_MANY_ROWS = 192;
 inline bool held_rows(const LogitRows &in) {
-    const int pieces = logits_pieces(in.n, in.bf16);
-    return pieces <= 1024 || (pieces <= 8192 && in.rows >= 192);
+    return logits_pieces(in.n, in.bf16) <= LOGITS_HELD_PIECES && (in.n <= LOGITS_HELD_FEW || in.rows >= LOGITS_MANY_ROWS);
 }
-inline bool small_parts(const LogitRows &in) {
+inline bool held_plain_rows(const LogitRows &in) {
+    return logits_pieces(in.n, in.bf16) <= LOGITS_HELD_PLAIN_PIECES && (in.n <= LOGITS_HELD_PLAIN_FEW || in.rows >= LOGITS_MANY_ROWS);
+}
+// Whether the parts are small: as long as they are few, of all rows and of each (what joins the row's parts takes longer with more).
+// Measured, large parts against small ones, in us: 1 x 131071 in bf16 loss 11.8 - 10.2, loss and gradient 18.3 - 14.3, plain
+// sampling 16.9 - 10.2; sampling with a histogram from each part 33.5 - 30.8 there (33 small parts), 30.6 - 33.5 in float32 (64),
+// and 30.5 - 39.1 for 1 x 250007 in float32 (123).
+constexpr int LOGITS_FEW_PARTS = 48;
+inline bool small_parts(const LogitRows &in, int most) {
     const int parts = logits_parts(logits_pieces(in.n, in.bf16), LOGITS_SMALL_PART_PIECES);
-    return parts <= LOGITS_MOST_PARTS && (long)in.rows * parts <= LOGITS_MOST_SMALL_PARTS;
+    return parts <= most && (long)in.rows * parts <= LOGITS_MOST_SMALL_PARTS;
 }
 // Rows that go out in one launch in parts (for both types alike): what a call needs of the workspace stays bounded.
 inline long rows_of_slice(int n) {

@@ -75,11 +75,18 @@ struct Draw {
     int k;
     bool first;  // the first of the order, whatever else is asked for
     __device__ __forceinline__ Draw(const SampleArgs &a, long r) {
-        temperature = a.temperature ? a.temperature[r] : 1.0f;
-        k = a.top_k && a.top_k[r] > 0 ? min(a.top_k[r], a.in.n) : a.in.n;
-        top_p = a.top_p ? a.top_p[r] : 1.0f;
-        min_p = a.min_p ? fminf(fmaxf(a.min_p[r], 0.0f), 1.0f) : 0.0f;
-        u = fminf(fmaxf(a.uniform[r], 0.0f), 1.0f - 5.9604645e-08f);  // (into [0, 1); NaN: 0)
+        // (all loaded, from some row of numbers or other, before one is looked at: a branch for each would wait for each)
+        const float *any = a.uniform;
+        u = any[r];
+        temperature = (a.temperature ? a.temperature : any)[r];
+        k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(any))[r];
+        top_p = (a.top_p ? a.top_p : any)[r];
+        min_p = (a.min_p ? a.min_p : any)[r];
+        u = fminf(fmaxf(u, 0.0f), 1.0f - 5.9604645e-08f);  // (into [0, 1); NaN: 0)
+        temperature = a.temperature ? temperature : 1.0f;
+        k = a.top_k && k > 0 ? min(k, a.in.n) : a.in.n;
+        top_p = a.top_p ? top_p : 1.0f;
+        min_p = a.min_p ? fminf(fmaxf(min_p, 0.0f), 1.0f) : 0.0f;
         first = !(temperature > 0.0f);
         if (first) temperature = 1.0f, k = 1, top_p = 1.0f, min_p = 0.0f;
     }
@@ -376,11 +383,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_join_kernel(SampleArgs a,
     constexpr int BATCH = 16;  // (their loads are on the way together)
     for (int first = 0; first < parts; first += BATCH) {
         u64 v[BATCH];
+        const int p_lane = min(first + (int)(threadIdx.x & (BATCH - 1)), parts - 1), down_lane = down[p_lane], used_lane = used[p_lane];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int p = first + i, b = p < parts ? (int)threadIdx.x - down[p] : -1;
+            const int b = (int)threadIdx.x - read_lane(down_lane, i);
             v[i] = 0;
-            if (b >= 0 && b < used[min(p, parts - 1)]) v[i] = in[p].weight[b];
+            if (first + i < parts && b >= 0 && b < read_lane(used_lane, i)) v[i] = in[first + i].weight[b];
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) count[0] += packed.count(v[i]), lacking[0] += packed.lack(v[i]);
@@ -595,6 +603,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
                                [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
 }
 
+bool cuts(const SampleArgs &a) { return a.top_k || a.top_p || a.min_p; }
+
 // most: rows of a launch.
 template <typename T, int PIECES>
 hipError_t launch_parts(const SampleArgs &a, int pieces, long most, char *ws, hipStream_t s) {
@@ -602,7 +612,7 @@ hipError_t launch_parts(const SampleArgs &a, int pieces, long most, char *ws, hi
     SampleRow *rows = reinterpret_cast<SampleRow *>(ws);
     SamplePart *sums = reinterpret_cast<SamplePart *>(ws + most * sizeof(SampleRow));
     return by_slices(a.in.rows, most, [&](int r, int n) {
-        if (a.top_k || a.top_p || a.min_p) {
+        if (cuts(a)) {
             sample_part_kernel<T, PIECES, true><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums);
             sample_join_kernel<<<n, JOIN_THREADS, 0, s>>>(a, r, parts, sums, rows);
             sample_gather_kernel<T, PIECES><<<n * parts, PART_THREADS, 0, s>>>(a, r, parts, sums, rows);
@@ -617,11 +627,11 @@ hipError_t launch_parts(const SampleArgs &a, int pieces, long most, char *ws, hi
 template <typename T>
 hipError_t launch(const SampleArgs &a, char *ws, hipStream_t s) {
     const int pieces = logits_pieces(a.in.n, a.in.bf16);
-    if (held_rows(a.in))
+    if (cuts(a) ? held_rows(a.in) : held_plain_rows(a.in))
         return by_size(pieces, [&](auto N, auto THREADS) {
             return by_slices(a.in.rows, (1l << 31) / THREADS, [&](int r, int n) { sample_held_kernel<T, decltype(N)::value, decltype(THREADS)::value><<<n, (int)THREADS, 0, s>>>(a, r); });
         });
-    if (small_parts(a.in)) return launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s);
+    if (small_parts(a.in, cuts(a) ? LOGITS_FEW_PARTS : LOGITS_MOST_PARTS)) return launch_parts<T, LOGITS_SMALL_PART_PIECES>(a, pieces, a.in.rows, ws, s);
     return launch_parts<T, LOGITS_PART_PIECES>(a, pieces, rows_of_slice(a.in.n) < a.in.rows ? rows_of_slice(a.in.n) : a.in.rows, ws, s);
 }
 

@@ -12,10 +12,10 @@ namespace {
 
 constexpr int TOP_LIST = 2 * LOGITS_MAX_TOP;
 
-// A key that at least k of the keys reach (KEY_NONE + 1 if fewer are above that of -inf), close to the largest such.  By one wave, on
-// keys in LDS, `each` a lane.
+// A key that at least k of the keys reach (KEY_NONE + 1 if fewer are above that of -inf), close to the largest such.  For a whole wave, on
+// keys in LDS, EACH a lane.
 template <int EACH>
-__device__ uint32_t reached_by(const uint32_t *keys, int k) {
+__device__ __forceinline__ uint32_t reached_by(const uint32_t *keys, int k) {
     uint32_t own[EACH], low = 0xFFFFFFFFu, high = 0;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
@@ -52,9 +52,39 @@ struct Order {
 __device__ __forceinline__ u64 entry_of(uint32_t key, int j) { return (u64)key << 32 | (uint32_t)~j; }
 __device__ __forceinline__ uint32_t entry_key(u64 v) { return (uint32_t)(v >> 32); }
 
+// put(place, entry) for every logit of the row that is at least z_low, which becomes -inf there.  n: LDS, how many (also those beyond
+// TOP_LIST, which are not put).
+template <typename T, int N, typename F>
+__device__ __forceinline__ void take_out(HeldRow<T, N> &row, float z_low, int &n, F put) {
+    constexpr int PER = HeldRow<T, N>::PER;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < row.rounds) {
+            float v[PER];
+            unpack<T>(row.raw[i], v);
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) any |= v[e] >= z_low;
+            if (any) {
+                uint32_t some = 0;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) some |= v[e] >= z_low ? 1u << e : 0u;
+                int at = atomicAdd(&n, __popc(some));
+                const uint4 r = row.raw[i];
+#pragma unroll
+                for (int e = 0; e < PER; ++e) v[e] = some >> e & 1 ? -INFINITY : v[e];
+                row.raw[i] = pack<T>(v);
+                for (; some; some &= some - 1, ++at) {
+                    const int e = __ffs(some) - 1;
+                    if (at < TOP_LIST) put(at, entry_of(order_key(element<T>(r, e)), row.index(i) + e));
+                }
+            }
+        }
+}
+
 // Ranks the list (n entries) and writes the first k as the row's answer; adds the others' weights to outside, theirs to inside.
 template <int THREADS>
-__device__ void write_first(const TopArgs &a, long r, Order &o, int n, const Weight &weight, bool infinite, double &inside, double &outside) {
+__device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, int n, const Weight &weight, bool infinite, double &inside, double &outside) {
     auto put = [&](int rank, u64 v) {
         const float z = key_value(entry_key(v));
         const double w = exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
@@ -67,11 +97,15 @@ __device__ void write_first(const TopArgs &a, long r, Order &o, int n, const Wei
         }
     };
     if (n <= 256) {
-        for (int i = threadIdx.x; i < n; i += THREADS) {
+        // counted by as many neighbouring lanes for an entry as there are threads for
+        const int by = n * 16 <= THREADS ? 16 : n * 4 <= THREADS ? 4 : 1, lane = threadIdx.x & (by - 1);
+        for (int i = threadIdx.x / by; i < n; i += THREADS / by) {
             const u64 v = o.entry[i];
             int rank = 0;
-            for (int e = 0; e < n; ++e) rank += o.entry[e] > v;
-            put(rank, v);
+#pragma unroll 4
+            for (int e = lane; e < n; e += by) rank += o.entry[e] > v;
+            for (int d = 1; d < by; d *= 2) rank += __shfl_xor(rank, d);
+            if (lane == 0) put(rank, v);
         }
     } else {
         int size = 512;
@@ -93,9 +127,9 @@ __device__ void write_first(const TopArgs &a, long r, Order &o, int n, const Wei
 }
 
 // The list from a source with more than TOP_LIST logits that reach the bound: exactly the first k; the rest's weights as they are
-// below the cut, from the whole row.
+// below the cut, from the whole row.  n: how many reach the bound.
 template <int THREADS, typename T>
-__device__ __noinline__ void list_exactly(const TopArgs &a, const Row<T> &row, Order &o, uint32_t low, int n, const Weight &weight, bool infinite, double *outside) {
+__device__ __forceinline__ void list_exactly(const TopArgs &a, const Row<T> &row, Order &o, uint32_t low, int n, const Weight &weight, bool infinite, double *outside) {
     __syncthreads();
     if (threadIdx.x == 0) o.s.before = 0, o.s.weight_before = 0, o.s.inside = n, o.n = 0;
     __syncthreads();
@@ -114,7 +148,7 @@ __device__ __noinline__ void list_exactly(const TopArgs &a, const Row<T> &row, O
 }
 
 template <typename T, int N, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS < 1024 ? 6 : 4) void top_held_kernel(TopArgs a, int row0) {
+__global__ __launch_bounds__(THREADS, THREADS < 1024 ? 8 : 4) void top_held_kernel(TopArgs a, int row0) {
     __shared__ Order o;
     __shared__ double part[2][16];
     const long r = (long)row0 + blockIdx.x;
@@ -138,27 +172,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 6 : 4) void top_held_kern
     const bool infinite = key_value(best) == INFINITY;
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     // what reaches the bound is listed and taken out of the row
-    const float z_low = key_value(bound);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < row.rounds) {
-            constexpr int PER = HeldRow<T, N>::PER;
-            float v[PER];
-            unpack<T>(row.raw[i], v);
-            bool some = false;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) some |= v[e] >= z_low;
-            if (some) {
-#pragma unroll
-                for (int e = 0; e < PER; ++e)
-                    if (v[e] >= z_low) {
-                        const int at = atomicAdd(&o.n, 1);
-                        if (at < TOP_LIST) o.entry[at] = entry_of(order_key(v[e]), row.index(i) + e);
-                        v[e] = -INFINITY;
-                    }
-                row.raw[i] = pack<T>(v);
-            }
-        }
+    take_out(row, key_value(bound), o.n, [&](int at, u64 v) { o.entry[at] = v; });
     __syncthreads();
     double inside = 0.0, outside = 0.0;
     const int n = o.n;
@@ -187,9 +201,13 @@ struct TopPart {
     double outside;  // weights of the rest, at the part's own maximum
     uint32_t best;   // key of the maximum
     uint32_t bound;  // k logits of the part reach it, if it has as many
+    uint32_t bound_some;  // share_of() logits of it do
     int n;           // listed; more than TOP_LIST: the list is not complete
     u64 entry[TOP_LIST];
 };
+
+// A part's share of the first k, twice: half of the parts have k logits above a bound that each reaches with so many.
+__device__ __forceinline__ int share_of(int k, int parts) { return (2 * k + parts - 1) / parts; }
 
 template <typename T>
 __global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int row0, int parts, TopPart *out) {
@@ -216,119 +234,130 @@ __global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int r
     }
     if (threadIdx.x == 0) o.n = 0;
     __syncthreads();
-    if (wave == 0) {
-        const uint32_t bound = each == 8   ? reached_by<PART_THREADS / 64>(o.maxima, a.k)
-                               : each == 4 ? reached_by<2 * PART_THREADS / 64>(o.maxima, a.k)
-                               : each == 2 ? reached_by<4 * PART_THREADS / 64>(o.maxima, a.k)
-                                           : reached_by<8 * PART_THREADS / 64>(o.maxima, a.k);
-        if (lane == 0) o.bound = bound;
+    __shared__ uint32_t bound_some;
+    if (wave < 2) {  // (side by side)
+        const int k = wave == 0 ? a.k : share_of(a.k, parts);
+        const uint32_t bound = each == 8   ? reached_by<PART_THREADS / 64>(o.maxima, k)
+                               : each == 4 ? reached_by<2 * PART_THREADS / 64>(o.maxima, k)
+                               : each == 2 ? reached_by<4 * PART_THREADS / 64>(o.maxima, k)
+                                           : reached_by<8 * PART_THREADS / 64>(o.maxima, k);
+        if (lane == 0) (wave == 0 ? o.bound : bound_some) = bound;
     }
     best = wave_all(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
     __shared__ uint32_t part_k[PART_THREADS / 64];
     if (lane == 0) part_k[wave] = best;
     __syncthreads();
     best = across_waves<PART_THREADS / 64>(part_k, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
-    const float z_low = key_value(o.bound);
     TopPart &mine = out[blockIdx.x];
-#pragma unroll
-    for (int i = 0; i < PART_ROUNDS; ++i)
-        if (i < row.rounds) {
-            float v[PER];
-            unpack<T>(row.raw[i], v);
-            bool some = false;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) some |= v[e] >= z_low;
-            if (some) {
-#pragma unroll
-                for (int e = 0; e < PER; ++e)
-                    if (v[e] >= z_low) {
-                        const int at = atomicAdd(&o.n, 1);
-                        if (at < TOP_LIST) mine.entry[at] = entry_of(order_key(v[e]), row.index(i) + e);
-                        v[e] = -INFINITY;
-                    }
-                row.raw[i] = pack<T>(v);
-            }
-        }
+    take_out(row, key_value(o.bound), o.n, [&](int at, u64 v) { mine.entry[at] = v; });
     const bool infinite = key_value(best) == INFINITY;
     if (infinite) row.only_infinite();
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     double outside = 0.0;
     row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
     outside = block_sum<PART_THREADS>(outside, part_d);
-    if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.n = o.n;
+    if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.bound_some = bound_some, mine.n = o.n;
 }
 
-// The logits that a row's parts have listed.
-struct PartLists {
-    const TopPart *parts;
+// A list in LDS.
+struct ListSource {
+    const u64 *entry;
     int n;
     template <typename F>
     __device__ __forceinline__ void each_from(float z_low, F f) const {
         const uint32_t low = order_key(z_low);
-        for (int p = threadIdx.x >> 6; p < n; p += JOIN_THREADS / 64)
-            for (int i = threadIdx.x & 63; i < parts[p].n; i += 64) {
-                const u64 v = parts[p].entry[i];
-                if (entry_key(v) >= low) f(key_value(entry_key(v)), (int)~(uint32_t)v);
-            }
+        for (int i = threadIdx.x; i < n; i += JOIN_THREADS)
+            if (entry_key(entry[i]) >= low) f(key_value(entry_key(entry[i])), (int)~(uint32_t)entry[i]);
     }
 };
 
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int row0, int parts, const TopPart *in) {
-    __shared__ Order o;
+    __shared__ Order o, first;
+    __shared__ SearchLds s;
+    __shared__ int listed[LOGITS_MOST_PARTS];
+    constexpr int EACH = (LOGITS_MOST_PARTS + 63) / 64;
+    __shared__ uint32_t some[EACH * 64];
     __shared__ uint32_t part_k[2][JOIN_THREADS / 64];
-    __shared__ int part_n[2][JOIN_THREADS / 64];
+    __shared__ int part_n[JOIN_THREADS / 64];
     __shared__ double part_d[2][JOIN_THREADS / 64];
     const long r = (long)row0 + blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     in += (long)blockIdx.x * parts;
-    uint32_t best = 0, bound = 0;
-    int n = 0, most = 0;
-    if ((int)threadIdx.x < parts) best = in[threadIdx.x].best, bound = in[threadIdx.x].bound, n = most = in[threadIdx.x].n;  // (129 parts at most)
+    uint32_t best = 0, bound = 0, own_best = 0;
+    int most = 0;
+    double own_outside = 0.0;
+    if ((int)threadIdx.x < parts) {
+        const TopPart &p = in[threadIdx.x];
+        own_best = best = p.best, bound = p.bound, own_outside = p.outside, most = p.n;
+        listed[threadIdx.x] = min(most, TOP_LIST);
+    }
+    if (threadIdx.x < EACH * 64) some[threadIdx.x] = (int)threadIdx.x < parts ? in[threadIdx.x].bound_some : KEY_NONE;
+    if (threadIdx.x == 0) o.n = 0, first.n = 0;
     auto larger = [](uint32_t p, uint32_t q) { return p > q ? p : q; };
-    auto more = [](int p, int q) { return p > q ? p : q; };
-    best = block_all<JOIN_THREADS>(best, part_k[0], larger);
-    bound = block_all<JOIN_THREADS>(bound, part_k[1], larger);  // (k logits of one part reach it)
-    most = block_all<JOIN_THREADS>(most, part_n[0], more);
-    n = block_sum<JOIN_THREADS>(n, part_n[1]);
+    best = wave_all(best, larger), bound = wave_all(bound, larger), most = wave_all(most, [](int p, int q) { return p > q ? p : q; });
+    if (lane == 0) part_k[0][wave] = best, part_k[1][wave] = bound, part_n[wave] = most;
+    __syncthreads();
+    best = across_waves<JOIN_THREADS / 64>(part_k[0], larger);
+    bound = across_waves<JOIN_THREADS / 64>(part_k[1], larger);  // (k logits of one part reach it)
+    const int share = share_of(a.k, parts);
+    bound = max(bound, reached_by<EACH>(some, (a.k + share - 1) / share));  // (that many parts, with so many each)
+    most = across_waves<JOIN_THREADS / 64>(part_n, [](int p, int q) { return p > q ? p : q; });
     const bool infinite = key_value(best) == INFINITY;
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
-    double inside = 0.0, outside = 0.0;
-    const PartLists lists{in, parts};
-    if (most > TOP_LIST) {  // (a part with many equal logits)
+    auto weigh = [&](uint32_t key) { return exp2_64<11>(weight.log2_of(infinite ? as_infinite(key_value(key)) : key_value(key))); };
+    double inside = 0.0, outside = own_outside > 0.0 ? own_outside * weigh(own_best) : 0.0;
+    // what the parts have listed and reaches the largest of their bounds
+    if (most <= TOP_LIST) {
+        int shift = 6;  // each part's list in so many places, four of them loaded at once
+        while (1 << shift < most) ++shift;
+        for (int i0 = threadIdx.x; i0 < parts << shift; i0 += 4 * JOIN_THREADS) {
+            u64 v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = i0 + e * JOIN_THREADS, p = min(i >> shift, parts - 1), at = i & ((1 << shift) - 1);
+                const bool there = i >> shift < parts && at < listed[p];
+                v[e] = in[p].entry[there ? at : 0];
+                v[e] = there ? v[e] : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t key = entry_key(v[e]);
+                if (key >= bound) {
+                    const int at = atomicAdd(&o.n, 1);
+                    if (at < TOP_LIST) o.entry[at] = v[e];
+                } else if (key > 0) {
+                    outside += weigh(key);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const int n = o.n;
+    Order *list = &o;
+    if (most > TOP_LIST || n > TOP_LIST) {  // (many equal logits)
         const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
-        // (no logits are missing above the largest bound of an incomplete list, but which that is is not worth a search here)
-        uint32_t ordered = 0;
-        whole.each([&](float z, int) { ordered += z > -INFINITY; });
+        uint32_t reaching = 0;
+        whole.each([&](float z, int) { reaching += z > -INFINITY && order_key(z) >= bound; });
+        reaching = block_sum<JOIN_THREADS>(reaching, part_k[0]);
+        list_exactly<JOIN_THREADS>(a, whole, o, bound, (int)reaching, weight, infinite, &outside);
+    } else if (n > 256 && n > a.k) {  // (ranking so many costs more than a cut)
+        if (threadIdx.x == 0) s.before = 0, s.weight_before = 0, s.inside = n;
         __syncthreads();
-        ordered = block_sum<JOIN_THREADS>(ordered, part_k[1]);
-        list_exactly<JOIN_THREADS>(a, whole, o, KEY_NONE + 1, (int)ordered, weight, infinite, &outside);
-        n = o.n;
-    } else {
-        if ((int)threadIdx.x < parts && in[threadIdx.x].outside > 0.0) {
-            const float z = key_value(in[threadIdx.x].best);
-            outside = in[threadIdx.x].outside * exp2_64<11>(weight.log2_of(infinite ? as_infinite(z) : z));
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) o.s.before = 0, o.s.weight_before = 0, o.s.inside = n, o.n = 0;
-        __syncthreads();
-        Cut cut = keep_all();
-        if (n > MEMBERS && n > a.k) {  // (ranking more costs more than a histogram)
-            const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
-            cut = cut_among<JOIN_THREADS, false>(lists, whole, weight, o.s, Limit{(uint32_t)a.k, INFINITY}, bound, best, 0);
-            __syncthreads();
-        }
-        lists.each_from(-3.4028234663852886e38f, [&](float z, int j) {
+        const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
+        const ListSource source{o.entry, n};
+        const Cut cut = cut_among<JOIN_THREADS, false>(source, whole, weight, s, Limit{(uint32_t)a.k, INFINITY}, bound, best, 0);
+        source.each_from(key_value(bound), [&](float z, int j) {
             const uint32_t k = order_key(z);
             if (cut.keeps(k, j))
-                o.entry[min(atomicAdd(&o.n, 1), TOP_LIST - 1)] = entry_of(k, j);
+                first.entry[min(atomicAdd(&first.n, 1), TOP_LIST - 1)] = entry_of(k, j);
             else
-                outside += exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
+                outside += weigh(k);
         });
         __syncthreads();
-        n = o.n;
+        list = &first;
     }
-    write_first<JOIN_THREADS>(a, r, o, n, weight, infinite, inside, outside);
+    write_first<JOIN_THREADS>(a, r, *list, list->n, weight, infinite, inside, outside);
     if (!a.rest) return;
     inside = wave_sum(inside), outside = wave_sum(outside);
     if (lane == 0) part_d[0][wave] = inside, part_d[1][wave] = outside;

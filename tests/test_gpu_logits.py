@@ -54,10 +54,9 @@ def sample(ctx, view, u, **params):
     return classes.cpu().numpy(), logs.cpu().numpy()
 
 
-def check_sample(ctx, z, view, u, what, **params):
+def check_sample(ctx, z, view, u, what, only=None, **params):
     classes, logs = sample(ctx, view, u, **params)
-    rows = z.shape[0]
-    for r in range(rows):
+    for r in only or range(z.shape[0]):
         p = {k: float(np.float32(v[r])) for k, v in params.items() if v is not None}
         want, log = L.sample_row(z[r], float(np.float32(u[r])), T=p.get("temperature", 1.0), top_k=int(p.get("top_k", 0)),
                                  top_p=p["top_p"] if "top_p" in p and p["top_p"] == p["top_p"] else 1.0,
@@ -124,14 +123,14 @@ def test_sample_every_draw_of_a_row(ctx):
         check_sample(ctx, z, put(z, "fp32"), u, "every draw", **params)
 
 
-def check_top(ctx, z, view, k, T, what):
+def check_top(ctx, z, view, k, T, what, only=None):
     rows, n = z.shape
     values = torch.full((rows, k), math.nan, device="cuda")
     classes = torch.full((rows, k), -7, dtype=torch.int32, device="cuda")
     rest = torch.full((rows,), math.nan, device="cuda")
     ctx.sushi_top_logits(view, values, classes, rest, temperature=T, workspace=workspace(rows, n))
     values, classes, rest = values.cpu().numpy(), classes.cpu().numpy(), rest.cpu().numpy()
-    for r in range(rows):
+    for r in only or range(rows):
         want = L.top_row(z[r], k, float(np.float32(T)))
         assert np.array_equal(classes[r], want[1]), (what, r)
         assert np.array_equal(values[r], want[0].astype(np.float32)), (what, r)
@@ -179,7 +178,7 @@ def teacher_of(z, k, seed, T, spoil=False):
     return values.astype(np.float32), classes.astype(np.int32), rest.astype(np.float32)
 
 
-def check_distill(ctx, z, dtype, teacher, T, what, weight=None, in_place=False, stride=None, offset=0, forward_only=False):
+def check_distill(ctx, z, dtype, teacher, T, what, weight=None, in_place=False, stride=None, offset=0, forward_only=False, only=None):
     values, classes, rest = teacher
     rows, n = z.shape
     view = put(z, dtype, stride, offset)
@@ -189,7 +188,7 @@ def check_distill(ctx, z, dtype, teacher, T, what, weight=None, in_place=False, 
                       weight=floats(weight), grad=None if forward_only else grad, workspace=workspace(rows, n))
     loss, grad = loss.cpu().numpy().astype(np.float64), grad.float().cpu().numpy().astype(np.float64)
     T = float(np.float32(T))
-    for r in range(rows):
+    for r in only or range(rows):
         want, g, size = L.distill_row(z[r], values[r], classes[r], 0.0 if rest is None else float(rest[r]), T)
         # R is off by 5e-9 of itself at most, and with it ln S, and rest * ln R
         ok = loss[r] == want or (math.isnan(loss[r]) and math.isnan(want)) or abs(loss[r] - want) <= 2.0 ** -24 * abs(want) + 2e-8
@@ -234,6 +233,28 @@ def test_distill_contents(ctx, dtype, kind, n):
                 print("distill", dtype, kind, n, k, spoil, flush=True)
                 check_distill(ctx, z, dtype, (values, classes, rest), T, (kind, n, k, spoil))
                 check_distill(ctx, z, dtype, (values, classes, None), T, (kind, n, k, spoil, "no rest"))
+
+
+# long rows: held where there are many, in small parts where there are few, in large parts; in one launch and in several
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(2, 32003), (200, 15001), (200, 31001), (200, 65001), (70, 70001), (2, 1 << 20), (70, 1 << 20)])
+def test_forms_of_long_rows(ctx, dtype, rows, n):
+    z2 = rows_of("peaks", 2, n, dtype, n + rows)
+    values, classes, rest = teacher_of(z2, 40, n, 1.0)
+    turn = np.arange(rows) % 2
+    z, values, classes, rest = z2[turn], values[turn], classes[turn], rest[turn]
+    only = sorted({0, 1, rows // 2, 62 % rows, 63 % rows, 64 % rows, rows - 1})
+    view, u, f = put(z, dtype), np.random.default_rng(n).random(rows), filters(rows, n)
+    for names in SETS:
+        print("forms", dtype, rows, n, names, flush=True)
+        check_sample(ctx, z, view, u, (rows, n, names), only=only, **{k: v for k, v in f.items() if k in names})
+    for k in (1, 40, 1024):
+        print("forms, top", dtype, rows, n, k, flush=True)
+        check_top(ctx, z, view, k, 1.0, (rows, n, k), only=only)
+    del view
+    for more in (dict(), dict(in_place=True), dict(forward_only=True)):
+        print("forms, distill", dtype, rows, n, more, flush=True)
+        check_distill(ctx, z, dtype, (values, classes, rest), 1.0, (rows, n, more), only=only, **more)
 
 
 def test_distill_teachers_at_their_ends(ctx):
