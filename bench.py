@@ -16,6 +16,7 @@ Prints ONE JSON line: queries/s over the timed steps, plus
 """
 import argparse
 import json
+import math
 import os
 import sys
 import time
@@ -87,6 +88,9 @@ def main():
     ap.add_argument("--measure-table", action="store_true",
                     help="latency-target stream: measure the latency table in this run even if a frozen one is shipped")
     ap.add_argument("--table-runs", type=int, default=3, help="runs per table entry when it is measured")
+    ap.add_argument("--accuracy", choices=["size", "measured"], default="size",
+                    help="latency-target stream: the accuracies that Algorithm 1 decides from.  size = synthetic, growing with the "
+                         "SubNet's bytes; measured = exp(-divergence) of every SubNet's answers from the largest SubNet's")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-roofline", action="store_true")
     ap.add_argument("--no-latency", action="store_true", help="skip the lone-query latency passes")
@@ -153,7 +157,7 @@ def main():
     torch.cuda.synchronize()
 
     levels = None
-    table_info = None
+    table_info = agreed = None
     if by_target:
         # Algorithm 1 in the loop: the latency table L[SubNet][cached SubGraph] measured on this GPU (frozen
         # to a file when one is shipped for this workload), synthetic accuracies that grow with SubNet size
@@ -162,6 +166,11 @@ def main():
         acc = [0.0] * len(pool)
         for rank, i in enumerate(sorted(range(len(pool)), key=lambda i: sizes[i])):
             acc[i] = float(np.float32(0.70 + 0.01 * rank))
+        if args.accuracy == "measured":
+            largest = max(range(len(pool)), key=lambda i: sizes[i])
+            divergence, agreement = sushiabs.measure_agreement(ctx, pool, pool[largest], xs[res_list[0]], arch.n_classes)
+            acc = [float(np.float32(math.exp(-d))) for d in divergence]
+            agreed = [round(float(a), 4) for a in agreement]
         tpath = sushiabs.table_path(args.workload, budget, teams)
         frozen = sushiabs.load_table(tpath, len(pool), len(cands)) if mode == 3 and not args.measure_table else None
         if frozen is not None:
@@ -354,7 +363,7 @@ def main():
                       "teams_per_xcd": teams, "sgs": args.sgs, "Q": Q, "budget_bytes": budget,
                       "cold_sweep": bool(args.cold_sweep),
                       "distinct_subnets": len(distinct), "candidate_subgraphs": len(cands),
-                      "latency_table": table_info,
+                      "latency_table": table_info, **({"agreement_with_largest": agreed} if agreed else {}),
                       "subnets_served": len(served) if by_target else len({c.key() for c in serving})},
            "p50_latency_ms": p50_ms, "p50_latency_ms_mode0": p50_mode0_ms,
            "weight_bytes_per_query": dstat["weight_bytes_total"] / nq,

@@ -1820,11 +1820,27 @@ bool words(std::initializer_list<const void *> needed, std::initializer_list<con
 // Bytes from the first logit of the first row to the last of the last.
 size_t extent(const LogitRows &in, long stride) { return ((size_t)(in.rows - 1) * stride + in.n) * (in.bf16 ? 2 : 4); }
 
+// The context's device is the current one while this lives; then the caller's is again.
+struct CurrentDevice {
+    int before = -1;
+    hipError_t enter(int device) {
+        int now = -1;
+        hipError_t e = hipGetDevice(&now);
+        if (e != hipSuccess || now == device) return e;
+        if ((e = hipSetDevice(device)) == hipSuccess) before = now;
+        return e;
+    }
+    ~CurrentDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
 // Runs an operator's launches on the context's stream, between events if timing is on.
 template <typename F>
 int run_operator(sushi_ctx *c, int kc, double bytes, double flops, F launch) {
     hipError_t e;
-    if ((e = hipSetDevice(c->device)) != hipSuccess) return hip_fail(c, e, "hipSetDevice");
+    CurrentDevice current;
+    if ((e = current.enter(c->device)) != hipSuccess) return hip_fail(c, e, "hipSetDevice");
     c->stream_dirty = true;
     sushi_ctx::Pending pend{};
     if (c->timing) {

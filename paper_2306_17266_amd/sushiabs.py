@@ -13,6 +13,9 @@ L[i][j] is the latency of serving SubNet i while SubGraph j is cached; the extra
 
 Both only marshal calls into the library and do arithmetic on its answers; tables are frozen as
 JSON so that the library's scheduler and any reference scheduler decide from identical numbers.
+
+Accuracies, the scheduler's other input, have no data set here.  measure_agreement puts a figure on
+every SubNet without labels: how far its answers are from the largest SubNet's on given inputs.
 """
 import json
 import os
@@ -112,3 +115,41 @@ def latency_levels(table, n_levels):
     col = np.asarray(table, dtype=np.float32)[:, -1]
     lo, hi = float(col.min()), float(col.max())
     return [float(np.float32(lo + (hi - lo) * k / (n_levels - 1))) for k in range(n_levels)]
+
+
+def measure_agreement(ctx, subnets, teacher, xs, n_classes, k=32, temperature=1.0, sampling=None, seed=0):
+    """How far the answers of every SubNet are from the teacher's (a SubNet of the same SuperNet: the largest) on the inputs
+    xs, device tensors [batch, res, res, channels] of the teacher's and the SubNets' resolution.  Two float32 arrays, an entry
+    per SubNet:
+      divergence  mean distillation loss against the teacher's k leading logits at the temperature (0: the same answers)
+      agreement   share of the inputs for which both draw the same class from the same random numbers, with sampling (keyword
+                  arguments of sushi_sample as numbers); None: for which their first classes are the same
+    exp(-divergence) serves as an accuracy of Algorithm 1."""
+    import torch
+    rows, k = sum(x.shape[0] for x in xs), min(k, n_classes)
+    dev = xs[0].device
+    empty = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=dev)
+    logits = [empty(rows, n_classes) for _ in range(len(subnets) + 1)]
+    values, classes, rest, loss = empty(rows, k), empty(rows, k, dtype=torch.int32), empty(rows), empty(rows)
+    answers = [empty(rows, dtype=torch.int32) for _ in logits]
+    uniform = torch.from_numpy(np.random.default_rng(seed).random(rows, dtype=np.float32)).to(dev)
+    sampling = {"temperature": 0.0} if sampling is None else sampling
+    sampling = {n: torch.full((rows,), v, dtype=torch.int32 if n == "top_k" else torch.float32, device=dev) for n, v in sampling.items()}
+    work = empty(B.sushi_logits_workspace(rows, n_classes), dtype=torch.uint8)
+    torch.cuda.synchronize(dev)       # (the context may have another stream)
+    for cfg, out in zip([teacher] + list(subnets), logits):
+        at = 0
+        for x in xs:
+            ctx.sushi_infer(cfg, x, out[at:at + x.shape[0]])
+            at += x.shape[0]
+    ctx.sushi_quiesce()               # (in exec mode 3 logits are there after this, and the GPU is free for what reads them)
+    for out, answer in zip(logits, answers):
+        ctx.sushi_sample(out, uniform, answer, workspace=work, **sampling)
+    ctx.sushi_top_logits(logits[0], values, classes, rest, temperature=temperature, workspace=work)
+    divergence, agreement = np.zeros(len(subnets), dtype=np.float32), np.zeros(len(subnets), dtype=np.float32)
+    for i, out in enumerate(logits[1:]):
+        ctx.sushi_distill(out, values, classes, loss, rest=rest, temperature=temperature, workspace=work)
+        ctx.sushi_synchronize()
+        divergence[i] = np.mean(loss.cpu().numpy(), dtype=np.float64)
+        agreement[i] = np.mean(answers[i + 1].cpu().numpy() == answers[0].cpu().numpy())
+    return divergence, agreement

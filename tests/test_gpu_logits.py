@@ -346,6 +346,53 @@ def test_a_run_of_them_after_queries(ctx):
     c.close()
 
 
+@pytest.mark.parametrize("mode", [0, 1])
+def test_measure_agreement(mode):
+    """Against the definitions, on the logits of the same queries: losses off as in check_distill, after a list rounded to 32 bits."""
+    from paper_2306_17266_amd import sushiabs
+    from tests.common import make_problem
+    from workloads import arch as A
+    from workloads import tensors as T
+    arch = A.tiny_arch()
+    blob, _ = make_problem(arch, 4, False)
+    stream = torch.cuda.Stream()
+    c = S.Sushi(0, stream.cuda_stream)
+    c.sushi_load_supernet(arch, blob, S.FP32)
+    c.sushi_set_option(S.OPT_EXEC_MODE, mode)
+    xs = [torch.from_numpy(T.make_input(4, i, b, 32, 3, False)).cuda() for i, b in enumerate((6, 1, 9))]
+    subnets = [A.min_cfg(arch, 32), A.max_cfg(arch, 32)]
+    torch.cuda.synchronize()
+    z = []
+    for cfg in subnets:
+        out = torch.empty(16, arch.n_classes, device="cuda")
+        torch.cuda.synchronize()
+        for x, at in zip(xs, (0, 6, 7)):
+            c.sushi_infer(cfg, x, out[at:at + len(x)])
+        c.sushi_synchronize()
+        z.append(out.cpu().numpy())
+    u = np.random.default_rng(5).random(16, dtype=np.float32)
+    for k, sampling in ((4, None), (64, dict(temperature=3.0, top_k=5, top_p=0.9, min_p=0.01))):
+        divergence, agreement = sushiabs.measure_agreement(c, subnets, subnets[1], xs, arch.n_classes, k, 2.0, sampling, seed=5)
+        s = dict(T=0.0) if sampling is None else dict(T=3.0, top_k=5, top_p=float(np.float32(0.9)), min_p=float(np.float32(0.01)))
+        answers = [[L.sample_row(row, float(u[r]), **s)[0] for r, row in enumerate(rows)] for rows in z]
+        for i, rows in enumerate(z):
+            losses = [L.distill_row(row, *L.top_row(z[1][r], min(k, arch.n_classes), 2.0), 2.0)[0] for r, row in enumerate(rows)]
+            assert abs(divergence[i] - np.mean(losses)) <= 1e-6 * (1 + np.mean(losses))
+            assert agreement[i] == np.float32(np.mean(np.equal(answers[i], answers[1])))
+        assert divergence[0] > 0.01 and divergence[1] < 1e-6 and agreement[1] == 1.0
+    c.close()
+
+
+@pytest.mark.parametrize("T", [1e-45, 1e-30, 1e30, 3e38])
+def test_temperatures_at_their_ends(ctx, T):
+    z = rows_of("peaks", 4, 1000, "fp32", 50)
+    z[1], z[2] = z[1, 0], -z[2]
+    check_top(ctx, z, put(z, "fp32"), 20, T, T)
+    values, classes, rest = teacher_of(z, 20, 50, 1.0)
+    for r in (rest, None):
+        check_distill(ctx, z, "fp32", (values, classes, r), T, T, forward_only=True)
+
+
 def _all_three(c, z, u, values, classes, out, work):
     c.sushi_sample(z, u, out["class"], out["log"], top_k=out["k"], top_p=out["p"], workspace=work)
     c.sushi_top_logits(z, out["values"], out["classes"], out["rest"], workspace=work)

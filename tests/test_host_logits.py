@@ -109,6 +109,21 @@ for rows, n in ((2 ** 31 - 1, 10), (5_000_000, 1000), (300_000, 1 << 20)):
 ''')
 
 
+def test_the_current_device_is_the_callers_again(tmp_path):
+    run(tmp_path, CALLS + '''
+now = ctypes.c_int()
+for mine, current in ((0, 0), (0, 1), (1, 0), (1, 1)):
+    h = S.Sushi(mine, 0)
+    fake.hipSetDevice(current)
+    for op in (sample, top, distill):
+        fake.fake_clear_log()
+        assert op(h=h._h) == 0
+        fake.hipGetDevice(ctypes.byref(now))
+        assert now.value == current
+        assert {line.split()[0] for line in fake.fake_log().decode().splitlines()} == {str(mine)}
+''')
+
+
 def test_operators_are_in_the_statistics(tmp_path):
     out = run(tmp_path, CALLS + '''
 ctx.sushi_set_option(S.OPT_KERNEL_TIMING, 1)
