@@ -88,13 +88,9 @@ __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, 
     auto put = [&](int rank, u64 v) {
         const float z = key_value(entry_key(v));
         const double w = exp2_64<6>(weight.log2_of(infinite ? as_infinite(z) : z));
-        if (rank < a.k) {
-            a.values[r * a.k + rank] = z;
-            a.classes[r * a.k + rank] = (int)~(uint32_t)v;
-            inside += w;
-        } else {
-            outside += w;
-        }
+        const bool in = rank < a.k;  // (a branch between two sums would put both into memory)
+        inside += in ? w : 0.0, outside += in ? 0.0 : w;
+        if (in) a.values[r * a.k + rank] = z, a.classes[r * a.k + rank] = (int)~(uint32_t)v;
     };
     if (n <= 256) {
         // counted by as many neighbouring lanes for an entry as there are threads for
