@@ -52,11 +52,14 @@ struct Order {
 __device__ __forceinline__ u64 entry_of(uint32_t key, int j) { return (u64)key << 32 | (uint32_t)~j; }
 __device__ __forceinline__ uint32_t entry_key(u64 v) { return (uint32_t)(v >> 32); }
 
-// put(place, entry) for every logit of the row that is at least z_low, which becomes -inf there.  n: LDS, how many (also those beyond
-// TOP_LIST, which are not put).
-template <typename T, int N, typename F>
-__device__ __forceinline__ void take_out(HeldRow<T, N> &row, float z_low, int &n, F put) {
+// put(place, entry) for every logit of the row that is at least z_low, which becomes -inf there; places in the order of threads and their
+// pieces (not of an atomic: sums over the list are the same in every run).  Only the first TOP_LIST are put.  Returns how many there
+// are.  part: LDS, an entry per wave.
+template <int THREADS, typename T, int N, typename F>
+__device__ __forceinline__ int take_out(HeldRow<T, N> &row, float z_low, int *part, F put) {
     constexpr int PER = HeldRow<T, N>::PER;
+    static_assert(N * PER <= 64, "a mark for each logit of a thread");
+    u64 marks = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < row.rounds) {
@@ -69,8 +72,21 @@ __device__ __forceinline__ void take_out(HeldRow<T, N> &row, float z_low, int &n
                 uint32_t some = 0;
 #pragma unroll
                 for (int e = 0; e < PER; ++e) some |= v[e] >= z_low ? 1u << e : 0u;
-                int at = atomicAdd(&n, __popc(some));
+                marks |= (u64)some << (i * PER);
+            }
+        }
+    const int own = __popcll(marks), upto = wave_scan(own);
+    if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = upto;
+    __syncthreads();
+    int at = sum_before<THREADS / 64>(part) + upto - own;
+    if (own > 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t some = (uint32_t)(marks >> (i * PER)) & ((1u << PER) - 1);
+            if (some) {
                 const uint4 r = row.raw[i];
+                float v[PER];
+                unpack<T>(r, v);
 #pragma unroll
                 for (int e = 0; e < PER; ++e) v[e] = some >> e & 1 ? -INFINITY : v[e];
                 row.raw[i] = pack<T>(v);
@@ -80,6 +96,7 @@ __device__ __forceinline__ void take_out(HeldRow<T, N> &row, float z_low, int &n
                 }
             }
         }
+    return sum_across<THREADS / 64>(part);
 }
 
 // Ranks the list (n entries) and writes the first k as the row's answer; adds the others' weights to outside, theirs to inside.
@@ -94,15 +111,18 @@ __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, 
     };
     if (n <= 256) {
         // counted by as many neighbouring lanes for an entry as there are threads for
-        const int by = n * 16 <= THREADS ? 16 : n * 4 <= THREADS ? 4 : 1, lane = threadIdx.x & (by - 1);
-        for (int i = threadIdx.x / by; i < n; i += THREADS / by) {
-            const u64 v = o.entry[i];
-            int rank = 0;
+        static_assert(THREADS >= 256, "a lane for an entry at least");
+        const int by = n * 16 <= THREADS ? 16 : n * 4 <= THREADS ? 4 : 1, lane = threadIdx.x & (by - 1), i = threadIdx.x / by;
+        const u64 v = o.entry[min(i, TOP_LIST - 1)];
+        int rank = 0;
+        if (i < n) {
 #pragma unroll 4
             for (int e = lane; e < n; e += by) rank += o.entry[e] > v;
             for (int d = 1; d < by; d *= 2) rank += __shfl_xor(rank, d);
-            if (lane == 0) put(rank, v);
         }
+        __syncthreads();
+        if (i < n && lane == 0) o.entry[rank] = v;
+        __syncthreads();
     } else {
         int size = 512;
         while (size < n) size *= 2;
@@ -117,8 +137,8 @@ __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, 
                 }
                 __syncthreads();
             }
-        for (int i = threadIdx.x; i < n; i += THREADS) put(i, o.entry[i]);
     }
+    for (int i = threadIdx.x; i < n; i += THREADS) put(i, o.entry[i]);  // (by rank: the sums are the same in every run)
     for (int i = n + threadIdx.x; i < a.k; i += THREADS) a.values[r * a.k + i] = -INFINITY, a.classes[r * a.k + i] = -1;
 }
 
@@ -153,7 +173,6 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 8 : 4) void top_held_kern
     float m = -INFINITY;
     row.each([&](float z, int) { m = fmaxf(m, z); });
     o.maxima[threadIdx.x] = order_key(m);
-    if (threadIdx.x == 0) o.n = 0;
     __syncthreads();
     if (wave == 0) {
         const uint32_t bound = reached_by<THREADS / 64>(o.maxima, a.k);
@@ -168,18 +187,19 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 8 : 4) void top_held_kern
     const bool infinite = key_value(best) == INFINITY;
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     // what reaches the bound is listed and taken out of the row
-    take_out(row, key_value(bound), o.n, [&](int at, u64 v) { o.entry[at] = v; });
+    __shared__ int part_n[THREADS / 64];
+    int n = take_out<THREADS>(row, key_value(bound), part_n, [&](int at, u64 v) { o.entry[at] = v; });
     __syncthreads();
     double inside = 0.0, outside = 0.0;
-    const int n = o.n;
     if (n > TOP_LIST) {
         const Row<T> whole(a.in, r, wave, THREADS / 64, lane);
         list_exactly<THREADS>(a, whole, o, bound, n, weight, infinite, &outside);
+        n = o.n;
     } else if (a.rest) {
         if (infinite) row.only_infinite();
         row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
     }
-    write_first<THREADS>(a, r, o, min(o.n, TOP_LIST), weight, infinite, inside, outside);
+    write_first<THREADS>(a, r, o, n, weight, infinite, inside, outside);
     if (!a.rest) return;
     inside = wave_sum(inside), outside = wave_sum(outside);
     if (lane == 0) part[0][wave] = inside, part[1][wave] = outside;
@@ -206,7 +226,7 @@ struct TopPart {
 __device__ __forceinline__ int share_of(int k, int parts) { return (2 * k + parts - 1) / parts; }
 
 template <typename T>
-__global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int row0, int parts, TopPart *out) {
+__global__ __launch_bounds__(PART_THREADS, 6) void top_part_kernel(TopArgs a, int row0, int parts, TopPart *out) {
     __shared__ Order o;
     __shared__ double part_d[PART_THREADS / 64];
     const long r = (long)row0 + blockIdx.x / parts;
@@ -228,7 +248,6 @@ __global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int r
             best = max(best, group), group = KEY_NONE;
         }
     }
-    if (threadIdx.x == 0) o.n = 0;
     __syncthreads();
     __shared__ uint32_t bound_some;
     if (wave < 2) {  // (side by side)
@@ -245,14 +264,17 @@ __global__ __launch_bounds__(PART_THREADS) void top_part_kernel(TopArgs a, int r
     __syncthreads();
     best = across_waves<PART_THREADS / 64>(part_k, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
     TopPart &mine = out[blockIdx.x];
-    take_out(row, key_value(o.bound), o.n, [&](int at, u64 v) { mine.entry[at] = v; });
+    __shared__ int part_n[PART_THREADS / 64];
+    const int n = take_out<PART_THREADS>(row, key_value(o.bound), part_n, [&](int at, u64 v) { mine.entry[at] = v; });
     const bool infinite = key_value(best) == INFINITY;
-    if (infinite) row.only_infinite();
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     double outside = 0.0;
-    row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
+    if (a.rest) {
+        if (infinite) row.only_infinite();
+        row.each([&](float z, int) { outside += exp2_64<6>(weight.log2_of(z)); });
+    }
     outside = block_sum<PART_THREADS>(outside, part_d);
-    if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.bound_some = bound_some, mine.n = o.n;
+    if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.bound_some = bound_some, mine.n = n;
 }
 
 // A list in LDS.
@@ -303,8 +325,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     auto weigh = [&](uint32_t key) { return exp2_64<11>(weight.log2_of(infinite ? as_infinite(key_value(key)) : key_value(key))); };
     double inside = 0.0, outside = own_outside > 0.0 ? own_outside * weigh(own_best) : 0.0;
-    // what the parts have listed and reaches the largest of their bounds
-    if (most <= TOP_LIST) {
+    auto each_listed = [&](auto f) {  // f(entry), of all parts
         int shift = 6;  // each part's list in so many places, four of them loaded at once
         while (1 << shift < most) ++shift;
         for (int i0 = threadIdx.x; i0 < parts << shift; i0 += 4 * JOIN_THREADS) {
@@ -317,17 +338,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
                 v[e] = there ? v[e] : 0;
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t key = entry_key(v[e]);
-                if (key >= bound) {
-                    const int at = atomicAdd(&o.n, 1);
-                    if (at < TOP_LIST) o.entry[at] = v[e];
-                } else if (key > 0) {
-                    outside += weigh(key);
-                }
-            }
+            for (int e = 0; e < 4; ++e)
+                if (v[e]) f(v[e]);
         }
-    }
+    };
+    // what reaches the bound
+    if (most <= TOP_LIST)
+        each_listed([&](u64 v) {
+            if (entry_key(v) >= bound) {
+                const int at = atomicAdd(&o.n, 1);
+                if (at < TOP_LIST) o.entry[at] = v;
+            } else {
+                outside += weigh(entry_key(v));
+            }
+        });
     __syncthreads();
     const int n = o.n;
     Order *list = &o;
@@ -345,10 +369,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
         const Cut cut = cut_among<JOIN_THREADS, false>(source, whole, weight, s, Limit{(uint32_t)a.k, INFINITY}, bound, best, 0);
         source.each_from(key_value(bound), [&](float z, int j) {
             const uint32_t k = order_key(z);
-            if (cut.keeps(k, j))
-                first.entry[min(atomicAdd(&first.n, 1), TOP_LIST - 1)] = entry_of(k, j);
-            else
-                outside += weigh(k);
+            if (cut.keeps(k, j)) first.entry[min(atomicAdd(&first.n, 1), TOP_LIST - 1)] = entry_of(k, j);
+        });
+        each_listed([&](u64 v) {  // (in an order that is the same in every run)
+            if (entry_key(v) >= bound && !cut.keeps(entry_key(v), (int)~(uint32_t)v)) outside += weigh(entry_key(v));
         });
         __syncthreads();
         list = &first;
