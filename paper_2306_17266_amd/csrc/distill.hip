@@ -29,9 +29,8 @@ struct RowSums {
     double inv_sum;     // 1 / S
     double list_scale;  // (1 - r) / sum of exp((t - max t) / T)
     double rest_scale;  // weight (1 / S - r / R) / T
+    double weight;      // divided by T; 0: the gradient is zero
     float best, list_best;
-    float weight;  // divided by T; 0: the gradient is zero
-    float pad;
 };
 
 // The row's list in LDS, with a mark for every class in [low, high): bit (class - origin) & mask.  Returns with *twice set if a class may
@@ -183,23 +182,35 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, cons
         if (threadIdx.x == 0) a.loss[r] = empty ? 0.0f : nan ? NAN : (float)loss;
     }
     const float w = empty ? 0.0f : row.weight;
-    const double inv_sum = 1.0 / sum, share = mass == 0.0 ? inv_sum : rest > 0.0 ? inv_sum - mass / rest : 0.0;
-    return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan ? NAN : w * inv_t * share, m, tm, (float)(w * inv_t), 0.0f};
+    const double inv_sum = 1.0 / sum, share = mass == 0.0 ? inv_sum : rest > 0.0 ? inv_sum - mass / rest : 0.0, scale = w * inv_t * share;
+    return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan || scale != scale ? NAN : fmin(fmax(scale, -1.7e308), 1.7e308), w * inv_t, m, tm};
 }
 
 // Gradient of a listed class.
 __device__ __forceinline__ float list_gradient(const RowSums &s, double inv_t, float z, float t) {
     const double e = exp2_64<11>(Terms(s.best, inv_t).log2_of(z)), p = exp2_64<11>(Terms(s.list_best, inv_t).log2_of(t)) * s.list_scale;
-    return (float)((e * s.inv_sum - p) * (double)s.weight);
+    return (float)((e * s.inv_sum - p) * s.weight);
 }
 
-// Gradients of the others.  Weights have 32 bits here: what a gradient of 32 bits is left with is the rounding of the exponent, 2^-24
-// of it thrice.
+// Gradients of the others, out * 2^((z - best) * scale).  Weights have 32 bits here: what a gradient of 32 bits is left with is the
+// rounding of the exponent, 2^-24 of it thrice.  Where the unlisted have next to nothing of the student and more of the teacher, out
+// is large and the weights too small for 32 bits: the exponent then counts from the logit whose gradient is about 1.
 struct GradientOf {
     float best, scale, out;
-    __device__ __forceinline__ GradientOf(const RowSums &s, double inv_t)
-        : best(s.best == INFINITY || s.weight == 0.0f ? 0.0f : s.best), scale((float)(1.4426950408889634074 * inv_t)),
-          out(s.weight == 0.0f ? 0.0f : (float)s.rest_scale) {}
+    __device__ __forceinline__ GradientOf(const RowSums &s, double inv_t) {
+        const bool zero = s.weight == 0.0;
+        double o = zero ? 0.0 : s.rest_scale;
+        best = s.best == INFINITY || zero ? 0.0f : s.best;
+        const double scale_64 = 1.4426950408889634074 * inv_t;
+        const double largest = 3.4028234663852886e38;  // (an infinite factor would make NaN of weights of zero)
+        scale = (float)fmin(scale_64, largest);
+        if (fabs(o) > 1.0) {
+            const float from = (float)fmin(fmax((double)best - log2_64(fabs(o)) / scale_64, -largest), largest);
+            const double moved = ((double)from - (double)best) * scale_64 + log2_64(fabs(o));
+            o = copysign(exp2_64<11>(moved), o), best = from;
+        }
+        out = o != o ? NAN : (float)fmin(fmax(o, -largest), largest);
+    }
     __device__ __forceinline__ float of(float z) const { return __builtin_amdgcn_exp2f((z - best) * scale) * out; }
 };
 
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
     if (!a.grad) return;
     // (the gradient may take the logits' place: every thread has passed a barrier since its logits were read)
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
-    const bool zero = s.weight == 0.0f;
+    const bool zero = s.weight == 0.0;
     if (zero) row.none();
     const GradientOf gradient(s, inv_t);
     T *piece = grad + row.index(0);
@@ -342,11 +353,11 @@ __global__ __launch_bounds__(THREADS) void distill_grad_kernel(DistillArgs a, in
         const int i = o * THREADS + threadIdx.x;
         counts[o] = i < a.k && entry_counts(list, i, low, high, twice);
         own[o] = 0.0f;
-        if (counts[o] && s.weight != 0.0f) own[o] = list_gradient(s, 1.0 / (double)a.temperature, ld1(row.x + list[i]), a.values[r * a.k + i]);
+        if (counts[o] && s.weight != 0.0) own[o] = list_gradient(s, 1.0 / (double)a.temperature, ld1(row.x + list[i]), a.values[r * a.k + i]);
     }
     __syncthreads();
     if (s.best == INFINITY) row.only_infinite();
-    const bool together = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0, zero = s.weight == 0.0f;
+    const bool together = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.x)) & 15) == 0, zero = s.weight == 0.0;
     const GradientOf gradient(s, 1.0 / (double)a.temperature);
     for (int i = 0; i < row.rounds; ++i) {
         float v[PER];

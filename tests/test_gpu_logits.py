@@ -8,12 +8,14 @@ import torch
 
 import paper_2306_17266_amd as S
 from oracle import logits_ref as L
-from tests.logits_cases import CONTENTS, rows_of
+from tests.logits_cases import CONTENTS, round_to as rows_of_type, rows_of
 
 pytestmark = pytest.mark.gpu
 
 TORCH = {"fp32": torch.float32, "bf16": torch.bfloat16}
 HALF_STEP = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8}
+# Below 2^-126 the steps are equal, 2^-126 times a step at 1 (2^-23, 2^-7): a value there is rounded by up to half of one.
+HALF_STEP_SMALL = {"fp32": 2.0 ** -150, "bf16": 2.0 ** -134}
 # one element, around pieces of 16 bytes, around a workgroup's width, classes of the SuperNets, one and several parts of a row
 SIZES = [1, 2, 3, 7, 8, 9, 10, 63, 257, 1000, 1023, 2049, 8193, 16385, 33333, 70001, 140003]
 
@@ -204,7 +206,7 @@ def check_distill(ctx, z, dtype, teacher, T, what, weight=None, in_place=False, 
         # exponential is off by a step, and two products are rounded; below 2^-126 it may be zero.  Then the type's rounding.
         with np.errstate(invalid="ignore"):
             x = np.minimum(np.abs(np.where(np.isfinite(z[r]), z[r].astype(np.float64) - np.max(z[r]), 0.0)) / T * 1.4427, 150.0)
-            off = size * (2.1 * x + 4.0) * 2.0 ** -24 + HALF_STEP[dtype] * np.abs(g) * 1.001 + abs(w) / T * 2.0 ** -125
+            off = size * (2.1 * x + 4.0) * 2.0 ** -24 + HALF_STEP[dtype] * np.abs(g) * 1.001 + abs(w) / T * 2.0 ** -125 + HALF_STEP_SMALL[dtype]
             bad = ~((np.abs(grad[r] - g) <= off) | (np.isnan(grad[r]) & np.isnan(g)))
         assert not bad.any(), (what, r, np.flatnonzero(bad)[:5], grad[r][bad][:5], g[bad][:5], off[bad][:5])
 
@@ -276,6 +278,25 @@ def test_distill_teachers_at_their_ends(ctx):
     assert not rest.any()
     check_distill(ctx, z, "bf16", (values, classes, rest), 1.0, "whole row")
     check_distill(ctx, z, "bf16", (values, classes, np.full(3, 0.5, np.float32)), 1.0, "mass outside a list of all classes")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(5, 1000), (5, 33333), (300, 5000)])
+def test_distill_students_sure_of_the_list(ctx, dtype, rows, n):
+    """The classes that are not listed have next to nothing, the teacher's mass outside its list all the same: weights far below
+    2^-126 of the largest are divided by their own sum."""
+    rng = np.random.default_rng(n)
+    values, classes, _ = teacher_of(rows_of("peaks", 2, n, dtype, n), 8, n, 1.0)
+    turn = np.arange(rows) % 2
+    values, classes = values[turn], classes[turn]
+    for gap, T in ((60, 1.0), (88, 1.0), (110, 1.0), (300, 1.0), (600, 1.0), (30, 0.1), (64, 0.1), (6, 0.01)):
+        z = rng.standard_normal((rows, n)).astype(np.float32) * np.float32(T)
+        z[np.arange(rows)[:, None], classes] += np.float32(gap)
+        z = rows_of_type(z, dtype)
+        for rest in (np.float32([0.3, 1e-6, 1.0]), None):
+            print("sure", dtype, n, gap, T, flush=True)
+            check_distill(ctx, z, dtype, (values, classes, None if rest is None else rest[np.arange(rows) % 3]), T, (n, gap, T),
+                          weight=np.float32([1.0, -1e-3, 1e4, 0.0])[np.arange(rows) % 4], only=list(range(min(rows, 12))))
 
 
 def test_distill_gradient_against_differences_of_the_loss(ctx):
@@ -383,14 +404,15 @@ def test_measure_agreement(mode):
     c.close()
 
 
-@pytest.mark.parametrize("T", [1e-45, 1e-30, 1e30, 3e38])
+@pytest.mark.parametrize("T", [1e-45, 1e-38, 1e-30, 1e30, 3e38])
 def test_temperatures_at_their_ends(ctx, T):
     z = rows_of("peaks", 4, 1000, "fp32", 50)
     z[1], z[2] = z[1, 0], -z[2]
     check_top(ctx, z, put(z, "fp32"), 20, T, T)
     values, classes, rest = teacher_of(z, 20, 50, 1.0)
     for r in (rest, None):
-        check_distill(ctx, z, "fp32", (values, classes, r), T, T, forward_only=True)
+        check_distill(ctx, z, "fp32", (values, classes, r), T, T, forward_only=T < 1e-38)  # (1 / T is not a float32 number there)
+        check_distill(ctx, z, "fp32", (values, classes, r), T, T, weight=np.float32([1e4, 1, 0, -1e-3]), forward_only=T < 1e-30)
 
 
 def _all_three(c, z, u, values, classes, out, work):
