@@ -1,4 +1,4 @@
-// Operators on rows of logits (row_order.hip, distill.hip): what their launchers take.
+// Operators on rows of logits (sample.hip, top_logits.hip, distill.hip): what their launchers take.
 //
 // The order of a row: value descending, index ascending; a NaN counts as -inf, and what is -inf belongs to no order.
 // The weight of a logit: exp((z - max z) / T).

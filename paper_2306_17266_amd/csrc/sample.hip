@@ -206,6 +206,8 @@ __device__ void first_beyond(const HeldRow<T, N> &row, const u64 (&own)[N], cons
 
 // ------------------------------------------------------------------ a row in the registers of a workgroup
 
+// 1 x 1000 with all filters: 7 us, 16 x 1000 without: 5 (a launch that does nothing takes 2 to 3): the histogram, two scans and the sums
+// wait for each other, a row being one workgroup's.  256 x 16000: 18 us, in parts 34.
 template <typename T, int N, int THREADS>
 __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, int row0) {
     __shared__ SearchLds s;
@@ -252,6 +254,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
 
 // ------------------------------------------------------------------ a row in parts
 
+// 512 x 100003 in float32, top_p, min_p and temperature: 126 us, in launches of 53, 14, 37 and 25.  The first reads the row (206 MB, floor
+// 41) and adds to a histogram in LDS, 17 instructions of 64 bits a logit; the third reads it again, at 6 TB/s, to list one interval's members:
+// the row fits no compute unit's registers.  1 x 131071 in bf16: 5, 12, 5 and 9 us, of which the second and the last are one workgroup's.
 constexpr int PART_THREADS = 256, JOIN_THREADS = 1024;
 constexpr int LIST = 4096;  // members of the interval in which a row is cut that are kept for its last step
 constexpr int MOST_PARTS = LOGITS_MOST_PARTS;

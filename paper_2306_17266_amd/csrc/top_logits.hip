@@ -99,6 +99,34 @@ __device__ __forceinline__ int take_out(HeldRow<T, N> &row, float z_low, int *pa
     return sum_across<THREADS / 64>(part);
 }
 
+// Sorts SIZE entries, largest first: a bitonic network.  The 64 pairs of a wave lie in 128 neighbouring entries while the distance is at
+// most 64: those steps need no barrier of the workgroup (64 x 2000, k = 1024: 36 us with one for each step and a pair at a time, 29.5 so).
+template <int THREADS, int SIZE>
+__device__ __forceinline__ void sort_entries(Order &o) {
+    constexpr int OWN = (SIZE / 2 + THREADS - 1) / THREADS;
+    for (int width = 2; width <= SIZE; width *= 2)
+        for (int d = width / 2; d > 0; d /= 2) {
+            u64 p[OWN], q[OWN];
+            int lo[OWN];
+#pragma unroll
+            for (int t = 0; t < OWN; ++t) {
+                const int i = min(t * THREADS + (int)threadIdx.x, SIZE / 2 - 1);
+                lo[t] = (i & ~(d - 1)) * 2 + (i & (d - 1));
+                p[t] = o.entry[lo[t]], q[t] = o.entry[lo[t] + d];
+            }
+#pragma unroll
+            for (int t = 0; t < OWN; ++t)
+                if (t * THREADS + (int)threadIdx.x < SIZE / 2) {
+                    const bool turn = (p[t] < q[t]) == ((lo[t] & width) == 0);
+                    o.entry[lo[t]] = turn ? q[t] : p[t], o.entry[lo[t] + d] = turn ? p[t] : q[t];
+                }
+            if (d > 64 || (d == 1 && width > 64))  // (the next step's distance: d / 2, or width)
+                __syncthreads();
+            else
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"), __builtin_amdgcn_wave_barrier();
+        }
+}
+
 // Ranks the list (n entries) and writes the first k as the row's answer; adds the others' weights to outside, theirs to inside.
 template <int THREADS>
 __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, int n, const Weight &weight, bool infinite, double &inside, double &outside) {
@@ -109,7 +137,7 @@ __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, 
         inside += in ? w : 0.0, outside += in ? 0.0 : w;
         if (in) a.values[r * a.k + rank] = z, a.classes[r * a.k + rank] = (int)~(uint32_t)v;
     };
-    if (n <= 256) {
+    if (n <= 256) {  // (64 x 1000, k = 64: 8.2 us, sorted 13.8; with more entries the sort is level or ahead)
         // counted by as many neighbouring lanes for an entry as there are threads for
         static_assert(THREADS >= 256, "a lane for an entry at least");
         const int by = n * 16 <= THREADS ? 16 : n * 4 <= THREADS ? 4 : 1, lane = threadIdx.x & (by - 1), i = threadIdx.x / by;
@@ -124,19 +152,16 @@ __device__ __forceinline__ void write_first(const TopArgs &a, long r, Order &o, 
         if (i < n && lane == 0) o.entry[rank] = v;
         __syncthreads();
     } else {
-        int size = 512;
-        while (size < n) size *= 2;
+        const int size = n <= 512 ? 512 : n <= 1024 ? 1024 : TOP_LIST;
         for (int i = n + threadIdx.x; i < size; i += THREADS) o.entry[i] = 0;
         __syncthreads();
-        for (int width = 2; width <= size; width *= 2)
-            for (int d = width / 2; d > 0; d /= 2) {
-                for (int i = threadIdx.x; i < size / 2; i += THREADS) {
-                    const int lo = (i & ~(d - 1)) * 2 + (i & (d - 1)), hi = lo + d;
-                    const u64 p = o.entry[lo], q = o.entry[hi];
-                    if ((p < q) == ((lo & width) == 0)) o.entry[lo] = q, o.entry[hi] = p;
-                }
-                __syncthreads();
-            }
+        if (size == 512)
+            sort_entries<THREADS, 512>(o);
+        else if (size == 1024)
+            sort_entries<THREADS, 1024>(o);
+        else
+            sort_entries<THREADS, TOP_LIST>(o);
+        __syncthreads();
     }
     for (int i = threadIdx.x; i < n; i += THREADS) put(i, o.entry[i]);  // (by rank: the sums are the same in every run)
     for (int i = n + threadIdx.x; i < a.k; i += THREADS) a.values[r * a.k + i] = -INFINITY, a.classes[r * a.k + i] = -1;
@@ -163,6 +188,9 @@ __device__ __forceinline__ void list_exactly(const TopArgs &a, const Row<T> &row
     __syncthreads();
 }
 
+// 2048 x 32001 in bf16, k = 64: 73 us, 131 MB, floor 26.  33 of it read the row and find the bound, 11 list and rank, 29 are the weights
+// of the rest: 16 instructions of 64 bits a logit, which is what bounds it (without `rest`: 44).  Rows follow each other in few
+// workgroups, the next one's loads ahead of this one's weights: 109 (128 registers); 1024 threads with half the pieces: 90.
 template <typename T, int N, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 8 : 4) void top_held_kernel(TopArgs a, int row0) {
     __shared__ Order o;
@@ -212,6 +240,10 @@ __global__ __launch_bounds__(THREADS, THREADS < 1024 ? 8 : 4) void top_held_kern
 
 constexpr int PART_THREADS = 256, PART_ROUNDS = LOGITS_PART_PIECES / PART_THREADS, JOIN_THREADS = 1024;
 
+// 3 x 200003 in float32, k = 100 (25 parts a row): 11 us, then 12 for the join of three workgroups, whose loads, list and ranks wait for
+// each other.  512 x 131071 in bf16, k = 16: 105 us, without `rest` 67 (floor 26).  80 registers, so that six workgroups share a compute
+// unit: with 143 for bf16, which is what the compiler takes by itself, 115 us.
+
 // What a part has of the first k: what reaches the k-th largest of its own pieces' maxima.
 struct TopPart {
     double outside;  // weights of the rest, at the part's own maximum
@@ -233,7 +265,8 @@ __global__ __launch_bounds__(PART_THREADS, 6) void top_part_kernel(TopArgs a, in
     const int part = blockIdx.x % parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     HeldRow<T, PART_ROUNDS> row(a.in, r, wave, PART_THREADS / 64, lane, part * LOGITS_PART_PIECES, LOGITS_PART_PIECES);
     constexpr int PER = HeldRow<T, PART_ROUNDS>::PER;
-    // groups of 8, 4, 2 pieces or 1 of a thread: three times as many as k, if there are
+    // groups of 8, 4, 2 pieces or 1 of a thread: three times as many as k, if there are (the bound is loose with fewer, and finding
+    // it takes longer with more)
     const int each = 3 * a.k <= PART_THREADS ? 8 : 3 * a.k <= 2 * PART_THREADS ? 4 : 3 * a.k <= 4 * PART_THREADS ? 2 : 1;
     uint32_t best = KEY_NONE, group = KEY_NONE;
 #pragma unroll
@@ -277,22 +310,9 @@ __global__ __launch_bounds__(PART_THREADS, 6) void top_part_kernel(TopArgs a, in
     if (threadIdx.x == 0) mine.outside = outside, mine.best = best, mine.bound = o.bound, mine.bound_some = bound_some, mine.n = n;
 }
 
-// A list in LDS.
-struct ListSource {
-    const u64 *entry;
-    int n;
-    template <typename F>
-    __device__ __forceinline__ void each_from(float z_low, F f) const {
-        const uint32_t low = order_key(z_low);
-        for (int i = threadIdx.x; i < n; i += JOIN_THREADS)
-            if (entry_key(entry[i]) >= low) f(key_value(entry_key(entry[i])), (int)~(uint32_t)entry[i]);
-    }
-};
-
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int row0, int parts, const TopPart *in) {
-    __shared__ Order o, first;
-    __shared__ SearchLds s;
+    __shared__ Order o;
     __shared__ int listed[LOGITS_MOST_PARTS];
     constexpr int EACH = (LOGITS_MOST_PARTS + 63) / 64;
     __shared__ uint32_t some[EACH * 64];
@@ -311,7 +331,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
         listed[threadIdx.x] = min(most, TOP_LIST);
     }
     if (threadIdx.x < EACH * 64) some[threadIdx.x] = (int)threadIdx.x < parts ? in[threadIdx.x].bound_some : KEY_NONE;
-    if (threadIdx.x == 0) o.n = 0, first.n = 0;
+    if (threadIdx.x == 0) o.n = 0;
     auto larger = [](uint32_t p, uint32_t q) { return p > q ? p : q; };
     best = wave_all(best, larger), bound = wave_all(bound, larger), most = wave_all(most, [](int p, int q) { return p > q ? p : q; });
     if (lane == 0) part_k[0][wave] = best, part_k[1][wave] = bound, part_n[wave] = most;
@@ -325,7 +345,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
     const Weight weight(infinite ? 0.0f : key_value(best), 1.0 / (double)a.temperature);
     auto weigh = [&](uint32_t key) { return exp2_64<11>(weight.log2_of(infinite ? as_infinite(key_value(key)) : key_value(key))); };
     double inside = 0.0, outside = own_outside > 0.0 ? own_outside * weigh(own_best) : 0.0;
-    auto each_listed = [&](auto f) {  // f(entry), of all parts
+    // what the parts have listed and reaches the bound
+    if (most <= TOP_LIST) {
         int shift = 6;  // each part's list in so many places, four of them loaded at once
         while (1 << shift < most) ++shift;
         for (int i0 = threadIdx.x; i0 < parts << shift; i0 += 4 * JOIN_THREADS) {
@@ -339,45 +360,24 @@ __global__ __launch_bounds__(JOIN_THREADS) void top_join_kernel(TopArgs a, int r
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (v[e]) f(v[e]);
+                if (entry_key(v[e]) >= bound) {
+                    const int at = atomicAdd(&o.n, 1);
+                    if (at < TOP_LIST) o.entry[at] = v[e];
+                } else if (v[e]) {
+                    outside += weigh(entry_key(v[e]));
+                }
         }
-    };
-    // what reaches the bound
-    if (most <= TOP_LIST)
-        each_listed([&](u64 v) {
-            if (entry_key(v) >= bound) {
-                const int at = atomicAdd(&o.n, 1);
-                if (at < TOP_LIST) o.entry[at] = v;
-            } else {
-                outside += weigh(entry_key(v));
-            }
-        });
+    }
     __syncthreads();
     const int n = o.n;
-    Order *list = &o;
     if (most > TOP_LIST || n > TOP_LIST) {  // (many equal logits)
         const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
         uint32_t reaching = 0;
         whole.each([&](float z, int) { reaching += z > -INFINITY && order_key(z) >= bound; });
         reaching = block_sum<JOIN_THREADS>(reaching, part_k[0]);
         list_exactly<JOIN_THREADS>(a, whole, o, bound, (int)reaching, weight, infinite, &outside);
-    } else if (n > 256 && n > a.k) {  // (ranking so many costs more than a cut)
-        if (threadIdx.x == 0) s.before = 0, s.weight_before = 0, s.inside = n;
-        __syncthreads();
-        const Row<T> whole(a.in, r, wave, JOIN_THREADS / 64, lane);
-        const ListSource source{o.entry, n};
-        const Cut cut = cut_among<JOIN_THREADS, false>(source, whole, weight, s, Limit{(uint32_t)a.k, INFINITY}, bound, best, 0);
-        source.each_from(key_value(bound), [&](float z, int j) {
-            const uint32_t k = order_key(z);
-            if (cut.keeps(k, j)) first.entry[min(atomicAdd(&first.n, 1), TOP_LIST - 1)] = entry_of(k, j);
-        });
-        each_listed([&](u64 v) {  // (in an order that is the same in every run)
-            if (entry_key(v) >= bound && !cut.keeps(entry_key(v), (int)~(uint32_t)v)) outside += weigh(entry_key(v));
-        });
-        __syncthreads();
-        list = &first;
     }
-    write_first<JOIN_THREADS>(a, r, *list, list->n, weight, infinite, inside, outside);
+    write_first<JOIN_THREADS>(a, r, o, o.n, weight, infinite, inside, outside);
     if (!a.rest) return;
     inside = wave_sum(inside), outside = wave_sum(outside);
     if (lane == 0) part_d[0][wave] = inside, part_d[1][wave] = outside;
