@@ -156,24 +156,19 @@ __device__ __forceinline__ void write_nothing(const SampleArgs &a, long r) {  //
     if (a.log_prob) a.log_prob[r] = -INFINITY;
 }
 
-// Sums of value(logit, index) by pieces and over what the workgroup holds; wave[w]: LDS, the part of wave w.  Only what is at least
-// z_low has a value; FEW: which is not much.
-template <int THREADS, bool FEW, typename T, int N, typename F>
-__device__ u64 sum_values(const HeldRow<T, N> &row, u64 (&own)[N], u64 *wave, float z_low, F value) {
+// Sums of value(logit, index) by pieces and over what the workgroup holds; wave[w]: LDS, the part of wave w.
+template <int THREADS, typename T, int N, typename F>
+__device__ u64 sum_values(const HeldRow<T, N> &row, u64 (&own)[N], u64 *wave, F value) {
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         own[i] = 0;
         if (i < row.rounds) {
             const int j = row.index(i);
-            if (FEW) {
-                from_piece<T>(row.raw[i], j, z_low, [&](float z, int at) { own[i] += value(z, at); });
-            } else {
-                float v[HeldRow<T, N>::PER];
-                unpack<T>(row.raw[i], v);
+            float v[HeldRow<T, N>::PER];
+            unpack<T>(row.raw[i], v);
 #pragma unroll
-                for (int e = 0; e < HeldRow<T, N>::PER; ++e) own[i] += value(v[e], j + e);
-            }
+            for (int e = 0; e < HeldRow<T, N>::PER; ++e) own[i] += value(v[e], j + e);
             apart();
         }
         sum += own[i];
@@ -224,7 +219,6 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
     const bool infinite = best == INFINITY;
     if (infinite) row.only_infinite(), best = 0.0f;
     Kept kept{Weight(best, inv_t), keep_all(), draw.t_min(), fraction_bits(a.in.n)};
-    bool few = false;
     if (draw.cuts(a.in.n)) {
         constexpr int OWN = BINS / THREADS;
         const Grid grid(best, inv_t, best);  // (the largest logit is place 0: a row of equal logits has exact sums, and its cut is where the count says)
@@ -244,11 +238,10 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
             Row<T> whole(a.in, r, wave, THREADS / 64, lane);
             if (infinite) whole.only_infinite();
             kept.cut = cut_among<THREADS, true>(row, whole, kept.weight, s, limit, f.low, f.high, kept.fraction);
-            few = s.before <= (uint32_t)a.in.n / 64;
         }
     }
     u64 own[N];
-    const u64 total = few ? sum_values<THREADS, true>(row, own, s.part64, key_value(kept.cut.key), kept) : sum_values<THREADS, false>(row, own, s.part64, -INFINITY, kept);
+    const u64 total = sum_values<THREADS>(row, own, s.part64, kept);
     first_beyond<THREADS>(row, own, s.part64, target_of(draw.u, total), kept, [&](float z, int j) { write_answer(a, r, j, kept.weight.log2_of(z), kept.fraction, total); });
 }
 
@@ -594,7 +587,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs 
     PartRow<T, PIECES, JOIN_THREADS> row = part_row<T, PIECES, JOIN_THREADS>(a, r, chosen);
     if (m == INFINITY) row.only_infinite();
     u64 own[(PIECES + JOIN_THREADS - 1) / JOIN_THREADS];
-    const u64 here = sum_values<JOIN_THREADS, false>(row, own, s.part64, -INFINITY, kept);
+    const u64 here = sum_values<JOIN_THREADS>(row, own, s.part64, kept);
     if (here == 0) {  // (a part whose weights are all below the point by themselves, if not by their sum: its largest)
         const float part_best = m == INFINITY ? 0.0f : in[chosen].best;
         int j = 0x7FFFFFFF;
