@@ -367,20 +367,20 @@ def test_a_run_of_them_after_queries(ctx):
     c.close()
 
 
-@pytest.mark.parametrize("mode", [0, 1])
-def test_measure_agreement(mode):
+@pytest.mark.parametrize("mode,dtype", [(0, "fp32"), (1, "fp32"), (0, "bf16"), (3, "bf16")])
+def test_measure_agreement(mode, dtype):
     """Against the definitions, on the logits of the same queries: losses off as in check_distill, after a list rounded to 32 bits."""
     from paper_2306_17266_amd import sushiabs
     from tests.common import make_problem
     from workloads import arch as A
     from workloads import tensors as T
     arch = A.tiny_arch()
-    blob, _ = make_problem(arch, 4, False)
+    blob, _ = make_problem(arch, 4, dtype == "bf16")
     stream = torch.cuda.Stream()
     c = S.Sushi(0, stream.cuda_stream)
-    c.sushi_load_supernet(arch, blob, S.FP32)
+    c.sushi_load_supernet(arch, blob, S.BF16 if dtype == "bf16" else S.FP32)
     c.sushi_set_option(S.OPT_EXEC_MODE, mode)
-    xs = [torch.from_numpy(T.make_input(4, i, b, 32, 3, False)).cuda() for i, b in enumerate((6, 1, 9))]
+    xs = [torch.from_numpy(T.make_input(4, i, b, 32, 3, dtype == "bf16")).cuda().to(TORCH[dtype]) for i, b in enumerate((6, 1, 9))]
     subnets = [A.min_cfg(arch, 32), A.max_cfg(arch, 32)]
     torch.cuda.synchronize()
     z = []
@@ -462,6 +462,37 @@ def test_captured_and_replayed(rows, n):
         torch.cuda.synchronize()
         for name in out:
             assert torch.equal(got[name], out[name]), (i, name)
+    c.close()
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn on one stream, with eager calls in the same workspace between them: as each by itself."""
+    stream = torch.cuda.Stream()
+    c = S.Sushi(0, stream.cuda_stream)
+    problems = [_problem(3, 90001, "fp32", 60), _problem(40, 1000, "bf16", 61)]
+    work = torch.full((max(S.sushi_logits_workspace(3, 90001), S.sushi_logits_workspace(40, 1000)),), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    want, graphs = [], []
+    for p in problems:
+        _all_three(c, *p, work)
+        torch.cuda.synchronize()
+        want.append({k: v.clone() for k, v in p[-1].items()})
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            _all_three(c, *p, work)
+    for i in range(4):
+        for p in problems:
+            for name in ("class", "log", "values", "classes", "rest", "loss", "grad"):
+                p[-1][name].fill_(-3)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graphs[i % 2].replay()
+            _all_three(c, *problems[i % 2], work)
+            graphs[1 - i % 2].replay()
+        torch.cuda.synchronize()
+        for p, w in zip(problems, want):
+            for name in w:
+                assert torch.equal(w[name], p[-1][name]), (i, name)
     c.close()
 
 
