@@ -1,21 +1,13 @@
-// Device-side helpers of the operators on logits: access to a row, order keys, weights, sums over waves and workgroups.
+// Device-side helpers of the operators on logits: access to a row, weights, sums over waves and workgroups.
 #pragma once
 
 #include "device_common.h"
+#include "logit_grid.h"
 #include "logits.h"
 
 namespace sushi {
 
-// ------------------------------------------------------------------ order and weight of a logit
-
-// Unsigned numbers in the order of the logits: larger = earlier.  NaN as -inf, -0 as 0.
-constexpr uint32_t KEY_NONE = 0x007FFFFFu;  // of -inf: in no order
-__device__ __forceinline__ uint32_t order_key(float z) {
-    z = z == z ? z + 0.0f : -INFINITY;
-    const uint32_t u = __float_as_uint(z);
-    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+// ------------------------------------------------------------------ weight of a logit (its order: logit_grid.h)
 
 // 2^t for t <= 0 in 64 bits: t = i + f with |f| <= 1/2, a polynomial for 2^f, and i into the exponent.  Below 2^-1022, for -inf
 // and for NaN: zero.  TERMS = 11: the power series, off by 2e-14 of the value at most.  TERMS = 6: for sums, off by 2e-9 at most; the

@@ -15,7 +15,6 @@ namespace sushi {
 
 typedef unsigned long long u64;
 
-constexpr int BINS = 1024;
 constexpr double LN2 = 6.931471805599453094e-01;
 constexpr int MEMBERS = 64;  // that one wave ranks, a lane each
 

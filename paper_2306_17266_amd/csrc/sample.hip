@@ -1,36 +1,13 @@
 // One class per row from given random numbers, under temperature, top-k, top-p and min-p (logits.h).
 //
 // The position at which top-k and top-p cut the order is searched with a histogram over a grid on the logits, 12 intervals for each
-// factor 2 of the weight, and then among the members of one interval (row_order.h).  The answer is found in the order of the
+// factor 2 of the weight (logit_grid.h), and then among the members of one interval (row_order.h).  The answer is found in the order of the
 // indexes: sums of the kept weights by waves and pieces, then the piece in which the running sum passes u times the whole.
 #include "row_order.h"
 
 namespace sushi {
 
 namespace {
-
-constexpr double BINS_PER_LOG2 = 12.0;  // 1024: down to 2^-85 of the largest weight, the rest in the last one
-
-// The grid: a logit lies in interval floor(place), counted downwards from the largest logit's.
-struct Grid {
-    double anchor, scale, top;  // place 0; intervals per unit of the logits; the largest logit's interval
-    // (rounded by itself: fused with a subtraction it would be another number in each use)
-    __device__ __forceinline__ double place(float z) const {
-#pragma clang fp contract(off)
-        return (anchor - (double)z) * scale;
-    }
-    __device__ __forceinline__ Grid(float best, double inv_t, double anchor_) : anchor(anchor_), scale(inv_t * (1.4426950408889634074 * BINS_PER_LOG2)) { top = floor(place(best)); }
-    // Key of the smallest logit in intervals 0 .. b.
-    __device__ __forceinline__ uint32_t lowest_key(int b, float best, double unit) const {  // unit: 1 / scale, about
-        const uint32_t lowest = KEY_NONE + 1, highest = order_key(best);
-        const double x = top + (b + 1.0);
-        if (b >= BINS - 1 || !(scale > 0.0)) return lowest;
-        uint32_t k = order_key((float)fmin(fmax(anchor - x * unit, -3.4028234663852886e38), 3.4028234663852886e38));
-        while (k > lowest && place(key_value(k - 1)) < x) --k;
-        while (k < highest && place(key_value(k)) >= x) ++k;
-        return k;
-    }
-};
 
 // An interval of the grid's histogram in one word: how many, above the sum of what their weights lack of the interval's upper end
 // (relative to it, 1 - 2^(-1/12) = 0.056 at most), in fixed point.
@@ -126,7 +103,7 @@ __device__ Range search(SearchLds &s, const Grid &grid, const Packed &packed, fl
     const int end = bin == stop ? max(stop_end, bin) : bin;
     const double unit = (double)draw.temperature * (LN2 / BINS_PER_LOG2);
     // (the lower and the upper end, in neighbouring lanes)
-    const uint32_t k = grid.lowest_key(threadIdx.x & 1 ? bin - 1 : end, best, unit);
+    const uint32_t k = lowest_key(grid, threadIdx.x & 1 ? bin - 1 : end, best, unit);
     const uint32_t low = read_lane(k, 0), above_high = read_lane(k, 1);
     if (end != bin && threadIdx.x == 0) s.inside = 0x7FFFFFFF;  // (more than is known)
     __syncthreads();
