@@ -77,23 +77,27 @@ def list_of(classes, n):
 
 
 def distill_row(z, values, classes, rest=0.0, T=1.0):
-    """(loss, gradient by z, for each class the sum of the magnitudes that the gradient is the difference of)."""
+    """(loss, gradient by z, for each class the sum of the magnitudes that the gradient is the difference of).  A loss beyond the
+    range of float32 is infinite, as in the operator's output."""
     z = np.asarray(z, dtype=np.float64)
     n = len(z)
     at = list_of(classes, n)
     c, t = np.asarray(classes)[at].astype(np.int64), np.asarray(values, dtype=np.float64)[at]
     rest = min(max(rest, 0.0), 1.0) if rest == rest else rest
     if np.isnan(z).any() or np.isnan(t).any() or rest != rest:
-        empty = False
         return math.nan, np.full(n, math.nan), np.full(n, math.nan)
-    empty = len(at) == 0 or t.max() == -np.inf or z.max() == -np.inf
-    if empty:
+    if len(at) == 0 or t.max() == -np.inf or z.max() == -np.inf:
         return 0.0, np.zeros(n), np.zeros(n)
     e = weights(z, T)
     total = e.sum()
-    listed = np.zeros(n, dtype=bool)
-    listed[c] = True
-    e_rest = e[~listed].sum()
+    others = np.ones(n, dtype=bool)
+    others[c] = False
+    # the mass outside the list by its own largest weight: relative to the row's largest it may be below 2^-1074
+    share, log_others = np.zeros(n), -math.inf  # of each class in the others' weight; ln of that weight
+    if others.any() and z[others].max() > -np.inf and (z.max() < np.inf or z[others].max() == np.inf):
+        e_others = weights(z[others], T)
+        share[others] = e_others / e_others.sum()
+        log_others = math.log(e_others.sum()) + ((z[others].max() - z.max()) / T if z.max() < np.inf else 0.0)
     p = weights(t, T)
     p = p / p.sum() * (1.0 - rest)
     # ln q from the differences, which do not underflow
@@ -101,10 +105,11 @@ def distill_row(z, values, classes, rest=0.0, T=1.0):
         log_q = (z[c] - z.max()) / T - math.log(total) if z.max() < np.inf else np.log(e[c] / total)
         loss = float(np.sum(np.where(p > 0, p * (np.log(np.where(p > 0, p, 1.0)) - log_q), 0.0)))
         if rest > 0:
-            loss += rest * (math.log(rest) - (math.log(e_rest / total) if e_rest > 0 else -math.inf))
-    share = 1.0 / total - (rest / e_rest if rest > 0 and e_rest > 0 else 0.0)
-    grad = e * (share / T)
-    size = e / total / T + (e * (rest / e_rest) / T if rest > 0 and e_rest > 0 else 0.0)
+            loss += rest * (math.log(rest) - (log_others - math.log(total)))
+    if loss >= 3.4028235677973366e38:  # (half a step above the largest float32)
+        loss = math.inf
+    grad = (e / total - rest * share) / T
+    size = (e / total + rest * share) / T
     grad[c] = (e[c] / total - p) / T
     size[c] = (e[c] / total + p) / T
     return loss, grad, size

@@ -1,12 +1,14 @@
 // Distillation from a teacher's leading logits (logits.h): the loss of a row and its gradient.
 //
-//   q = softmax(z / T);  e_j = exp((z_j - max z) / T), S = their sum, R = their sum over the classes that are not listed
+//   q = softmax(z / T);  e_j = exp((z_j - max z) / T), S = their sum
+//   for the classes that are not listed, u = the largest of their logits:  f_j = exp((z_j - u) / T), R = their sum, A = exp((u - max z) / T)
 //   p_i = (1 - r) softmax(t / T) over the row's list, r = the mass outside it
-//   loss  = sum_i p_i (ln p_i - ln q_i) + r (ln r - ln(R / S))
-//   d loss / d z_j = (e_j / S - p_j) / T for a listed class, e_j (1 / S - r / R) / T for another
+//   loss  = sum_i p_i (ln p_i - ln q_i) + r (ln r - (u - max z) / T - ln R + ln S)
+//   d loss / d z_j = (e_j / S - p_j) / T for a listed class, f_j (A / S - r / R) / T for another
 //
-// The loss is a small difference of large terms where student and teacher agree, and R is a small part of S where both are sure:
-// R is summed by itself, never as S minus the list, and the sums, the list's terms and the logarithms have 64 bits.
+// The loss is a small difference of large terms where student and teacher agree: the unlisted weights are summed by themselves, never
+// as S minus the list, and the sums, the list's terms and the logarithms have 64 bits.  Where the student is sure of its list, A passes
+// below 2^-1074 (a gap of 745 T) while its logarithm and R, which is at least 1, are ordinary numbers.
 #include <algorithm>
 
 #include "logits_device.h"
@@ -21,16 +23,18 @@ constexpr double LN2 = 6.931471805599453094e-01;
 
 // What a part of a row adds to it, and what a row's loss and gradient need, in the workspace.
 struct PartSums {
-    double rest;  // sum of the weights of what is not listed, at the part's own maximum
-    float best;   // NaN if the part holds one
+    double rest;  // sum of the weights of what is not listed, relative to the largest of them in the part
+    float best;   // that logit; NaN if there is one among them
     float pad;
 };
 struct RowSums {
     double inv_sum;     // 1 / S
     double list_scale;  // (1 - r) / sum of exp((t - max t) / T)
-    double rest_scale;  // weight (1 / S - r / R) / T
+    double rest_scale;  // weight (A / S - r / R) / T
     double weight;      // divided by T; 0: the gradient is zero
     float best, list_best;
+    float rest_best;  // u, read as the row is (as_infinite)
+    float pad;
 };
 
 // The row's list in LDS, with a mark for every class in [low, high): bit (class - origin) & mask.  Returns with *twice set if a class may
@@ -62,7 +66,7 @@ __device__ __forceinline__ bool entry_counts(const int *list, int i, int low, in
 
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }  // (NaN if one is)
 
-// The maximum of this thread's logits, NaN if there is one.
+// The maximum of this thread's logits, NaN if there is one among them.
 template <typename R>
 __device__ __forceinline__ float own_largest(const R &row) {
     float m = -INFINITY;
@@ -124,26 +128,36 @@ __device__ __forceinline__ Entries<OWN> read_entries(const DistillArgs &a, long 
     return own;
 }
 
-// The maxima of the row (from each thread's own) and of its list.
+// The maxima of a row, of its unlisted logits, of the teacher's list.
+struct Maxima {
+    float row, rest, list;
+    // u, where the row is read as as_infinite() says if its maximum is infinite
+    __device__ __forceinline__ float anchor() const { return row == INFINITY ? as_infinite(rest) : rest; }
+};
+// m: of this thread's unlisted logits.  Only the waves that have entries look at them.
 template <int THREADS, int OWN>
-__device__ __forceinline__ void maxima(float &m, float &tm, const Entries<OWN> &own, float (*part)[THREADS / 64]) {
-    tm = -INFINITY;
+__device__ __forceinline__ Maxima maxima(float m, int k, const Entries<OWN> &own, float (*part)[THREADS / 64]) {
+    float z = -INFINITY, t = -INFINITY;
+    if ((int)(threadIdx.x & ~63u) < k) {
 #pragma unroll
-    for (int o = 0; o < OWN; ++o) tm = larger(tm, own.t[o]);
-    m = wave_all(m, larger), tm = wave_all(tm, larger);
-    if ((threadIdx.x & 63) == 0) part[0][threadIdx.x >> 6] = m, part[1][threadIdx.x >> 6] = tm;
+        for (int o = 0; o < OWN; ++o) z = larger(z, own.z[o]), t = larger(t, own.t[o]);
+        z = wave_all(z, larger), t = wave_all(t, larger);
+    }
+    m = wave_all(m, larger);
+    if ((threadIdx.x & 63) == 0) part[0][threadIdx.x >> 6] = m, part[1][threadIdx.x >> 6] = z, part[2][threadIdx.x >> 6] = t;
     __syncthreads();
-    m = across_waves<THREADS / 64>(part[0], larger), tm = across_waves<THREADS / 64>(part[1], larger);
+    m = across_waves<THREADS / 64>(part[0], larger);
+    return Maxima{larger(m, across_waves<THREADS / 64>(part[1], larger)), m, across_waves<THREADS / 64>(part[2], larger)};
 }
 
 // The row's loss (written) and what its gradient needs, from the maxima and each thread's part of R.  Only the waves that have
 // entries compute with them.
 template <int THREADS, int OWN>
-__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, const RowInputs &row, float m, float tm, double rest, const Entries<OWN> &own, double (*part)[THREADS / 64]) {
+__device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, const RowInputs &row, const Maxima &top, double rest, const Entries<OWN> &own, double (*part)[THREADS / 64]) {
     const int wave = threadIdx.x >> 6;
     const bool entries = wave * 64 < a.k;
     const double inv_t = 1.0 / (double)a.temperature;
-    const Terms student(m, inv_t), teacher(tm, inv_t);
+    const Terms student(top.row, inv_t), teacher(top.list, inv_t);
     double sum = 0.0, list_sum = 0.0;
     if (entries) {
 #pragma unroll
@@ -154,11 +168,13 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, cons
     rest = wave_sum(rest);
     if ((threadIdx.x & 63) == 0) part[0][wave] = rest, part[1][wave] = sum, part[2][wave] = list_sum;
     __syncthreads();
-    rest = sum_across<THREADS / 64>(part[0]), sum = rest + sum_across<THREADS / 64>(part[1]), list_sum = sum_across<THREADS / 64>(part[2]);
-    const bool nan = m != m || tm != tm;
+    const double log2_u = student.log2_of(top.rest), a_u = exp2_64<11>(log2_u);  // of A, A
+    rest = sum_across<THREADS / 64>(part[0]), list_sum = sum_across<THREADS / 64>(part[2]);
+    sum = rest * a_u + sum_across<THREADS / 64>(part[1]);
+    const bool nan = top.row != top.row || top.list != top.list;
     double mass = row.rest;  // outside the list
     mass = mass < 0.0 ? 0.0 : mass > 1.0 ? 1.0 : mass;
-    const bool empty = !nan && (m == -INFINITY || tm == -INFINITY);
+    const bool empty = !nan && (top.row == -INFINITY || top.list == -INFINITY);
     if (a.loss) {
         double loss = 0.0;
         if (entries) {
@@ -172,7 +188,7 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, cons
                     if (p != 0.0) loss += p * (log_p - (student.log2_of(own.z[o]) * LN2 - log_sum));
                 }
             loss = wave_sum(loss);
-            if (wave == 0 && mass != 0.0) loss += mass * ((log2_64(mass) - log2_64(rest)) * LN2 + log_sum);
+            if (wave == 0 && mass != 0.0) loss += mass * ((log2_64(mass) - log2_64(rest) - log2_u) * LN2 + log_sum);
         }
         if (a.k > 64) {
             if ((threadIdx.x & 63) == 0) part[3][wave] = loss;
@@ -182,8 +198,8 @@ __device__ __forceinline__ RowSums finish_row(const DistillArgs &a, long r, cons
         if (threadIdx.x == 0) a.loss[r] = empty ? 0.0f : nan ? NAN : (float)loss;
     }
     const float w = empty ? 0.0f : row.weight;
-    const double inv_sum = 1.0 / sum, share = mass == 0.0 ? inv_sum : rest > 0.0 ? inv_sum - mass / rest : 0.0, scale = w * inv_t * share;
-    return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan || scale != scale ? NAN : fmin(fmax(scale, -1.7e308), 1.7e308), w * inv_t, m, tm};
+    const double inv_sum = 1.0 / sum, share = mass == 0.0 ? a_u * inv_sum : rest > 0.0 ? a_u * inv_sum - mass / rest : 0.0, scale = w * inv_t * share;
+    return RowSums{nan ? NAN : inv_sum, (1.0 - mass) / list_sum, nan || scale != scale ? NAN : scale, w * inv_t, top.row, top.list, top.anchor(), 0.0f};
 }
 
 // Gradient of a listed class.
@@ -192,23 +208,16 @@ __device__ __forceinline__ float list_gradient(const RowSums &s, double inv_t, f
     return (float)((e * s.inv_sum - p) * s.weight);
 }
 
-// Gradients of the others, out * 2^((z - best) * scale).  Weights have 32 bits here: what a gradient of 32 bits is left with is the
-// rounding of the exponent, 2^-24 of it thrice.  Where the unlisted have next to nothing of the student and more of the teacher, out
-// is large and the weights too small for 32 bits: the exponent then counts from the logit whose gradient is about 1.
+// Gradients of the others, out * 2^((z - u) * scale).  Weights have 32 bits here: what a gradient of 32 bits is left with is the
+// rounding of the exponent, 2^-24 of it thrice, and what is 2^-126 of the row's largest is zero.
 struct GradientOf {
     float best, scale, out;
     __device__ __forceinline__ GradientOf(const RowSums &s, double inv_t) {
         const bool zero = s.weight == 0.0;
-        double o = zero ? 0.0 : s.rest_scale;
-        best = s.best == INFINITY || zero ? 0.0f : s.best;
-        const double scale_64 = 1.4426950408889634074 * inv_t;
         const double largest = 3.4028234663852886e38;  // (an infinite factor would make NaN of weights of zero)
-        scale = (float)fmin(scale_64, largest);
-        if (fabs(o) > 1.0) {
-            const float from = (float)fmin(fmax((double)best - log2_64(fabs(o)) / scale_64, -largest), largest);
-            const double moved = ((double)from - (double)best) * scale_64 + log2_64(fabs(o));
-            o = copysign(exp2_64<11>(moved), o), best = from;
-        }
+        best = s.rest_best == -INFINITY || zero ? 0.0f : s.rest_best;  // (-inf: there are no others above it, and they get 0)
+        scale = (float)fmin(1.4426950408889634074 * inv_t, largest);
+        const double o = zero ? 0.0 : s.rest_scale;
         out = o != o ? NAN : (float)fmin(fmax(o, -largest), largest);
     }
     __device__ __forceinline__ float of(float z) const { return __builtin_amdgcn_exp2f((z - best) * scale) * out; }
@@ -235,22 +244,21 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
     __shared__ uint32_t bits[SPAN / 32];
     __shared__ int list[LOGITS_MAX_TOP];
     __shared__ int twice;
-    __shared__ float part_f[2][THREADS / 64];
+    __shared__ float part_f[3][THREADS / 64];
     __shared__ double part_d[4][THREADS / 64];
     const long r = (long)row0 + blockIdx.x;
     HeldRow<T, N> row(a.in, r, threadIdx.x >> 6, THREADS / 64, threadIdx.x & 63);
     const RowInputs inputs(a, r);
     mark_list<THREADS>(a, r, 0, a.in.n, -row.lead, SPAN - 1, bits, list, &twice);
     const Entries<OWN> own = read_entries<T, THREADS, OWN>(a, r, list, twice);
-    float m = own_largest(row), tm;
-    maxima<THREADS>(m, tm, own, part_f);
-    const double inv_t = 1.0 / (double)a.temperature;
-    if (m == INFINITY) row.only_infinite();
     leave_unlisted(row, bits, -row.lead);
-    const Weight weight(m == INFINITY ? 0.0f : m, inv_t);
+    const Maxima top = maxima<THREADS>(own_largest(row), a.k, own, part_f);
+    const double inv_t = 1.0 / (double)a.temperature;
+    if (top.row == INFINITY) row.only_infinite();
+    const Weight weight(top.anchor(), inv_t);
     double rest = 0.0;
     row.each([&](float z, int) { rest += exp2_64<6>(weight.log2_of(z)); });
-    const RowSums s = finish_row<THREADS>(a, r, inputs, m, tm, rest, own, part_d);
+    const RowSums s = finish_row<THREADS>(a, r, inputs, top, rest, own, part_d);
     if (!a.grad) return;
     // (the gradient may take the logits' place: every thread has passed a barrier since its logits were read)
     T *grad = static_cast<T *>(a.grad) + r * a.grad_stride;
@@ -299,9 +307,9 @@ __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, in
     HeldRow<T, PIECES / THREADS> row(a.in, r, wave, THREADS / 64, lane, part * PIECES, PIECES);
     const int origin = part * SPAN - row.lead;
     mark_list<THREADS>(a, r, max(origin, 0), min(origin + SPAN, a.in.n), origin, SPAN - 1, bits, list, &twice);
+    leave_unlisted(row, bits, origin);
     const float m = block_all<THREADS>(own_largest(row), part_f, larger);
     if (m == INFINITY) row.only_infinite();
-    leave_unlisted(row, bits, origin);
     const Weight weight(m == INFINITY ? 0.0f : m, 1.0 / (double)a.temperature);
     double rest = 0.0;
     row.each([&](float z, int) { rest += exp2_64<6>(weight.log2_of(z)); });
@@ -314,7 +322,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     __shared__ uint32_t bits[LIST_BITS / 32];
     __shared__ int list[LOGITS_MAX_TOP];
     __shared__ int twice;
-    __shared__ float part_f[2][THREADS / 64];
+    __shared__ float part_f[3][THREADS / 64];
     __shared__ double part_d[4][THREADS / 64];
     constexpr int OWN = LOGITS_MAX_TOP / THREADS;
     const long r = (long)row0 + blockIdx.x;
@@ -325,14 +333,14 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
     mark_list<THREADS>(a, r, 0, n, 0, mask, bits, list, &twice);
     in += (long)blockIdx.x * parts;
     const Entries<OWN> own = read_entries<T, THREADS, OWN>(a, r, list, twice);
-    float m = -INFINITY, tm;
+    float m = -INFINITY;
     for (int p = threadIdx.x; p < parts; p += THREADS) m = larger(m, in[p].best);
-    maxima<THREADS>(m, tm, own, part_f);
-    const Terms student(m, 1.0 / (double)a.temperature);
+    const Maxima top = maxima<THREADS>(m, a.k, own, part_f);
+    const Weight weight(top.anchor(), 1.0 / (double)a.temperature);
     double rest = 0.0;
     for (int p = threadIdx.x; p < parts; p += THREADS)
-        if (in[p].rest != 0.0) rest += in[p].rest * exp2_64<11>(student.log2_of(in[p].best));
-    const RowSums s = finish_row<THREADS>(a, r, inputs, m, tm, rest, own, part_d);
+        if (in[p].rest != 0.0) rest += in[p].rest * exp2_64<11>(weight.log2_of(top.row == INFINITY ? as_infinite(in[p].best) : in[p].best));
+    const RowSums s = finish_row<THREADS>(a, r, inputs, top, rest, own, part_d);
     if (threadIdx.x == 0) out[blockIdx.x] = s;
 }
 
