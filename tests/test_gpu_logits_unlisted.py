@@ -21,9 +21,9 @@ def ctx():
     c.close()
 
 
-def check(ctx, z, dtype, values, classes, rest, T, weight, what, in_place=False, rows=None):
-    view = put(z, dtype)
-    loss, grad = torch.full((z.shape[0],), 7.0, device="cuda"), view if in_place else torch.full_like(view, 7.0)
+def check(ctx, z, dtype, values, classes, rest, T, weight, what, in_place=False, rows=None, view=None, grad=None):
+    view = put(z, dtype) if view is None else view
+    loss, grad = torch.full((z.shape[0],), 7.0, device="cuda"), view if in_place else torch.full_like(view, 7.0) if grad is None else grad
     ctx.sushi_distill(view, torch.from_numpy(values).cuda(), torch.from_numpy(classes).cuda(), loss, rest=floats(rest), temperature=T,
                       weight=floats(weight), grad=grad, workspace=workspace(*z.shape))
     loss, grad = loss.cpu().numpy().astype(np.float64), grad.float().cpu().numpy().astype(np.float64)
@@ -40,7 +40,7 @@ def check(ctx, z, dtype, values, classes, rest, T, weight, what, in_place=False,
         # each, the sums in the factor by 2e-9 each (0.1 half steps).  A weight below 2^-126 may be zero; a factor that small is rounded by
         # up to half of 2^-149.  A listed class has 64 bits.  Then the type's rounding.
         with np.errstate(invalid="ignore"):
-            x = np.where(others, np.abs(z[r].astype(np.float64) - z[r][others].max()), 0.0) / T * 1.4426950408889634
+            x = np.where(others, np.abs(z[r].astype(np.float64) - z[r][others].max(initial=-np.inf)), 0.0) / T * 1.4426950408889634
             x = np.where(np.isfinite(x), np.minimum(x, 150.0), 150.0)
             off = abs(w) * size * np.where(others, 2.1 * x + 4.1, 0.1) * 2.0 ** -24 + HALF_STEP[dtype] * np.abs(g * w) * 1.001
             off += abs(w) / T * 2.0 ** -125 + 2.0 ** -149 + HALF_STEP_SMALL[dtype]
