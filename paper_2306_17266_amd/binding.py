@@ -283,7 +283,7 @@ def _refuse(what):
 
 
 class Sushi:
-    """One context (device + stream)."""
+    """One context (device + stream).  Calls on one context must not overlap in time: threads have one each."""
 
     def __init__(self, device=0, stream=None):
         if device < 0:
@@ -407,7 +407,8 @@ class Sushi:
 
     # Operators on logits.  Device tensors in and out, as in sushi_infer: nothing is allocated, copied or converted here.
     # What the C call cannot see of a tensor (its device, its type, its strides) is checked first.  The structs are the
-    # context's own, filled again by every call.
+    # context's own, filled again by every call: as everywhere, calls on one context must not overlap in time, and threads
+    # need one each (or a lock around the whole call).
     def _operand(self, t, what, dtype, shape):
         """Address of a contiguous tensor of that type (a name) and shape; None: NULL."""
         if t is None:

@@ -235,7 +235,7 @@ __device__ __forceinline__ void store_elements(T *grad, int n, int j, uint4 r) {
 
 // For gradients whose rows lie to 16 bytes as those of the logits do.  The logits stay in registers as they came, and their weights are
 // computed again for the gradient: with 80 registers three workgroups of 512 share a compute unit, and one loads or stores while
-// another computes.  4096 x 32000 in bf16, loss and gradient: 139 us, 542 MB at 3.9 TB/s (a copy reaches 5.1: floor 103); with two
+// another computes.  4096 x 32000 in bf16, loss and gradient: 142 us, 542 MB at 3.8 TB/s (a copy reaches 5.1: floor 103); with two
 // workgroups a compute unit 147, with four 152 (spilled registers), weights kept from the loss for the gradient 199 against 154 then.
 // What is left is the loss: 25 instructions a logit that only partly run beside the loads and stores of other workgroups.
 template <typename T, int N, int THREADS>
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(THREADS, 6) void distill_held_kernel(DistillArgs a,
 
 // ------------------------------------------------------------------ a row in parts
 
-// 5 x 250007 in bf16, loss: 10.6 us; 4.7 for the parts and 6.7 for what a row's workgroup does with its list and sums, one wait
+// 5 x 250007 in bf16, loss: 10.7 us; 4.8 for the parts and 7 for what a row's workgroup does with its list and sums, one wait
 // after another.
 template <typename T, int PIECES>
 __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, int row0, int parts, PartSums *out) {
@@ -317,6 +317,8 @@ __global__ __launch_bounds__(THREADS) void distill_part_kernel(DistillArgs a, in
     if (threadIdx.x == 0) out[blockIdx.x] = PartSums{rest, m, 0.0f};
 }
 
+// Rows of more than LIST_BITS classes share marks: with 1024 of 2^20 classes one or two pairs usually do, and each entry is then compared with
+// those before it (4 x 1048576, loss: 181 us with 1024 entries, 13 with 64; 4 x 262144 with 1024: 12).
 template <typename T>
 __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int row0, int parts, const PartSums *in, RowSums *out) {
     __shared__ uint32_t bits[LIST_BITS / 32];
@@ -420,6 +422,8 @@ hipError_t launch_parts(const DistillArgs &a, int pieces, long most, char *ws, h
 template <typename T>
 hipError_t launch(const DistillArgs &a, char *ws, hipStream_t s) {
     const int pieces = logits_pieces(a.in.n, a.in.bf16);
+    // Gradients whose rows lie otherwise within 16 bytes are stored an element at a time, in parts: 256 x 1000 in float32 14 us against
+    // 8.5, 4096 x 32000 in bf16 313 against 155.
     const bool together = !a.grad || ((reinterpret_cast<uintptr_t>(a.grad) - reinterpret_cast<uintptr_t>(a.in.x)) % 16 == 0 &&
                                       (a.in.rows == 1 || (a.grad_stride - a.in.stride) * (long)sizeof(T) % 16 == 0));
     if (together && held_rows(a.in)) {

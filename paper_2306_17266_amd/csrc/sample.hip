@@ -224,11 +224,14 @@ __global__ __launch_bounds__(THREADS, 4) void sample_held_kernel(SampleArgs a, i
 
 // ------------------------------------------------------------------ a row in parts
 
-// 512 x 100003 in float32, top_p, min_p and temperature: 126 us, in launches of 53, 14, 37 and 25.  The first reads the row (206 MB, floor
+// 512 x 100003 in float32, top_p, min_p and temperature: 125 us, in launches of 53, 13, 37 and 25.  The first reads the row (206 MB, floor
 // 41) and adds to a histogram in LDS, 17 instructions of 64 bits a logit; the third reads it again, at 6 TB/s, to list one interval's members:
 // the row fits no compute unit's registers.  1 x 131071 in bf16: 5, 12, 5 and 9 us, of which the second and the last are one workgroup's.
 constexpr int PART_THREADS = 256, JOIN_THREADS = 1024;
-constexpr int LIST = 4096;  // members of the interval in which a row is cut that are kept for its last step
+// Members of the interval in which a row is cut that are kept for its last step.  Where it has more (flat rows, high temperatures, hundreds of
+// thousands of classes) the last launch's one workgroup reads the row itself for every step instead: normal logits, deviation 2.5, top_p
+// 0.95, 16 x 250007: 42 us at T = 1, 254 at T = 2; 4 x 1048576: 753 and 940.
+constexpr int LIST = 4096;
 constexpr int MOST_PARTS = LOGITS_MOST_PARTS;
 
 // What a part has of its row: its maximum and how often; the histogram over a grid that all parts of the row share (place 0 is the
@@ -474,7 +477,8 @@ struct Listed {
     }
 };
 
-// Last launch, a workgroup per row: the cut, the part in which the running sum passes the target, and the class there.
+// Last launch, a workgroup per row: the cut, the part in which the running sum passes the target, and the class there.  With 89
+// registers a compute unit has room for one workgroup (CUT): 512 rows take two rounds.
 template <typename T, int PIECES, bool CUT>
 __global__ __launch_bounds__(JOIN_THREADS) void sample_finish_kernel(SampleArgs a, int row0, int parts, const SamplePart *in, const SampleRow *rows) {
     __shared__ SearchLds s;
